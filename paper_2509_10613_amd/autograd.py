@@ -10,6 +10,12 @@ method happens here.
     loss = sig_mmd2(X, Y, lam1, lam2, flags)         # squared MMD between two sets of paths, one library call
     S = signature(x, N, flags)                       # x[B,L,d] -> truncated signatures [B, entries] (Section 2)
 
+and both ends of a model that is trained around them (include/sigtrain.h), for float64, float32, bfloat16 and float16:
+
+    x = embed(tokens, table, scale)                  # symbols [B,L] -> paths [B,L,d] of vectors from table[V,d]
+    loss = linear_cross_entropy(S, w, targets)       # read-out w[V,entries] of features, in pieces of the classes
+    norm = clip_grad_norm(grads, max_norm)           # all gradients of a step scaled down to a norm; grad_norm(grads)
+
 A time grid of the caller's own (Section 4 defines the time-augmented path as (x_{t_i}, t_i) and fixes no grid; the
 library's flag takes t_i = i/(L-1)) is an ordinary channel: ``with_times(x, t)`` appends it, and the wrappers below take
 ``times=`` / ``times_x=, times_y=`` and do that for the caller.
@@ -224,6 +230,84 @@ def signature(x, N, flags=0, times=None):
         x = with_times(x, times)
     out = _native.signature(x, N, flags)
     return _Signature.apply(x, N, flags) if out is None else out
+
+
+class _Embed(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, table, scale):
+        tokens = tokens.contiguous()
+        ctx.save_for_backward(tokens)
+        ctx.args = (table.shape[0], scale)
+        return sk.embed_fwd(tokens, table.contiguous(), scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_out):
+        (tokens,) = ctx.saved_tensors
+        return None, sk.embed_bwd(tokens, grad_out.contiguous(), *ctx.args), None
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, w, targets, reduction):
+        h, w, targets = h.contiguous(), w.contiguous(), targets.contiguous()
+        loss, lse, rows = sk.entropy_fwd(h, w, targets, reduction)
+        ctx.save_for_backward(h, w, targets, lse, rows)
+        ctx.reduction = reduction
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        gh, gw = sk.entropy_bwd(*ctx.saved_tensors, grad.contiguous(), ctx.reduction, ctx.needs_input_grad[0], ctx.needs_input_grad[1])
+        return gh, gw, None, None
+
+
+def embed(tokens, table, scale=1.0):
+    """scale * table[tokens], [..., D] for integer device tensors tokens[...] and table[V, D]: sequences of symbols [B, L] as the paths
+    [B, L, D] that the calls above take; differentiable in table (the rows of a symbol are summed in a fixed order).  A token
+    outside 0 .. V - 1 (padding) gives zeros and takes no part in the gradient."""
+    return _Embed.apply(tokens, table, float(scale))
+
+
+def linear_cross_entropy(h, weight, targets, reduction="mean"):
+    """Softmax cross entropy of the logits h weight^T, h[..., D], weight[V, D], targets[...]: the mean over the rows with a target (0 if there
+    are none), the sum, or with "none" every row's; differentiable in h and weight.  The logits of all classes never exist at
+    once, forward or backward.  A row whose target is outside 0 .. V - 1 has none: its loss and its gradient are 0, and what it holds
+    reaches nothing.  float32 (float64 for float64 arrays)."""
+    if h.shape[:-1] != targets.shape:
+        raise ValueError("h[..., D] and targets[...] expected, got %s and %s" % (tuple(h.shape), tuple(targets.shape)))
+    loss = _LinearCrossEntropy.apply(h.reshape(-1, h.shape[-1]), weight, targets.reshape(-1), reduction)
+    return loss.view(targets.shape) if reduction == "none" else loss
+
+
+def grad_norm(grads):
+    """The Euclidean norm of all entries of a tensor or of several (of any floating types and layouts, on one device), as a float64 [] on
+    the device."""
+    grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
+    return sk.grad_norm([g.detach().contiguous() for g in grads])
+
+
+def clip_grad_norm(grads, max_norm, out=None):
+    """Scales a tensor or several, taken together, down to the norm `max_norm` where theirs is larger, in place, or into the tensors
+    `out` (which may be of other floating types: the optimizer's copies); returns their norm, a float64 [] on the device, without waiting
+    for it.  Tensors whose norm is infinite or NaN are left (passed on) as they are.  No tensor may come twice in place.  Tensors of
+    other layouts than contiguous ones go through copies."""
+    grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
+    outs = grads if out is None else ([out] if isinstance(out, torch.Tensor) else list(out))
+    with torch.no_grad():
+        dense = [g.contiguous() for g in grads]
+        if out is None:
+            norm = sk.clip(dense, float(max_norm))
+            written = dense
+        else:
+            written = [o if o.is_contiguous() else torch.empty_like(o, memory_format=torch.contiguous_format) for o in outs]
+            norm = sk.clip(dense, float(max_norm), out=written)
+        for o, w in zip(outs, written):
+            if o is not w:
+                o.copy_(w)
+        torch.autograd.graph.increment_version(outs)
+    return norm
 
 
 def with_times(x, t):

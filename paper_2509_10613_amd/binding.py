@@ -48,6 +48,13 @@ EXPORTS = ["sigkernel_workspace_bytes", "sigkernel_workspace_least_bytes", "sigk
            "signature_length", "signature_workspace_bytes", "signature_fwd", "signature_describe",
            "signature_bwd_workspace_bytes", "signature_bwd", "signature_bwd_describe"]
 
+ST_F32, ST_F64, ST_BF16, ST_F16 = 0, 1, 2, 3   # element types of the operators of include/sigtrain.h
+ST_I32, ST_I64 = 0, 1
+ST_NONE, ST_MEAN, ST_SUM = 0, 1, 2
+TRAIN_EXPORTS = ["sigtrain_embed_fwd", "sigtrain_embed_bwd_workspace_bytes", "sigtrain_embed_bwd",
+                 "sigtrain_entropy_workspace_bytes", "sigtrain_entropy_fwd", "sigtrain_entropy_bwd",
+                 "sigtrain_clip_workspace_bytes", "sigtrain_grad_norm", "sigtrain_clip", "sigtrain_describe"]
+
 _lib = None
 
 
@@ -107,6 +114,20 @@ def load():
     lib.signature_bwd_workspace_bytes.argtypes = [i64, i64, i64, ci, ci, ci, ci]
     lib.signature_bwd.restype = ci
     lib.signature_bwd.argtypes = [vp, vp, vp, vp, i64, i64, i64, ci, ci, ci, vp, C.c_size_t, vp]
+    f64, sz = C.c_double, C.c_size_t
+    for name, restype, argtypes in (
+            ("sigtrain_embed_fwd", ci, [vp, vp, vp, i64, i64, i64, f64, ci, ci, vp]),
+            ("sigtrain_embed_bwd_workspace_bytes", sz, [i64, i64, i64, ci]),
+            ("sigtrain_embed_bwd", ci, [vp, vp, vp, i64, i64, i64, f64, ci, ci, vp, sz, vp]),
+            ("sigtrain_entropy_workspace_bytes", sz, [ci, i64, i64, i64, ci, ci]),
+            ("sigtrain_entropy_fwd", ci, [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, ci, ci, vp, sz, vp]),
+            ("sigtrain_entropy_bwd", ci, [vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, ci, ci, vp, sz, vp]),
+            ("sigtrain_clip_workspace_bytes", sz, [i64]),
+            ("sigtrain_grad_norm", ci, [vp, vp, vp, i64, vp, vp, sz, vp]),
+            ("sigtrain_clip", ci, [vp, vp, vp, vp, vp, i64, f64, vp, vp, sz, vp]),
+            ("sigtrain_describe", ci, [ci, i64, i64, i64, ci, sz, C.c_char_p, sz])):
+        getattr(lib, name).restype = restype
+        getattr(lib, name).argtypes = argtypes
     lib.sigkernel_last_error.restype = C.c_char_p
     lib.sigkernel_version.restype = C.c_char_p
     _lib = lib
@@ -380,3 +401,187 @@ def signature_bwd(x, grad_out, N, flags=0, sig=None, ws=None, grad_x=None):
     _check(load().signature_bwd(_ptr(x), _ptr(sig), _ptr(grad_out), _ptr(grad_x), B, L, d, N, flags, dt, _ptr(ws),
                                 ws.numel(), _stream()))
     return grad_x
+
+
+# ---------------------------------------------------------------- both ends of a model (include/sigtrain.h)
+_ST_TYPES = {torch.float32: ST_F32, torch.float64: ST_F64, torch.bfloat16: ST_BF16, torch.float16: ST_F16}
+_ST_INDEX = {torch.int32: ST_I32, torch.int64: ST_I64}
+_ST_REDUCTIONS = {"none": ST_NONE, "mean": ST_MEAN, "sum": ST_SUM}
+
+
+def _st_dt(t):
+    try:
+        return _ST_TYPES[t.dtype]
+    except KeyError:
+        raise TypeError("float64, float32, bfloat16 or float16 tensors expected, got %s" % t.dtype) from None
+
+
+def _st_it(t):
+    try:
+        return _ST_INDEX[t.dtype]
+    except KeyError:
+        raise TypeError("int32 or int64 symbols and targets expected, got %s" % t.dtype) from None
+
+
+def _together(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("tensors on different devices: %s and %s" % (first.device, t.device))
+
+
+def _scratch(nbytes, device, least=None):
+    """Scratch of one call's own, from the caching allocator (calls on different streams and captured graphs share none).  Where the
+    device has no room for it, half of it and so on down to least(), the least the call takes."""
+    size, few = max(int(nbytes), 256), None
+    while True:
+        try:
+            return torch.empty(size, dtype=torch.uint8, device=device)
+        except torch.OutOfMemoryError:
+            if few is None:
+                few = max(least(), 256) if least else size
+            if size <= few:
+                raise
+            size = max(size // 2, few)
+
+
+def embed_fwd(tokens, table, scale=1.0, out=None):
+    """out[..., :] = scale * table[tokens[...], :] for tokens of any shape and table[V, D]; zeros where a token is outside 0 .. V - 1."""
+    _dev(tokens, "tokens"); _dev(table, "table")
+    _together(table, tokens, out)
+    if table.dim() != 2:
+        raise ValueError("table must be [V, D], got %s" % (tuple(table.shape),))
+    V, D = table.shape
+    dt, it = _st_dt(table), _st_it(tokens)
+    if out is None:
+        out = torch.empty((*tokens.shape, D), dtype=table.dtype, device=table.device)
+    elif tuple(_dev(out, "out").shape) != (*tokens.shape, D) or out.dtype != table.dtype:
+        raise ValueError("out must be %s of %s" % ((*tokens.shape, D), table.dtype))
+    with torch.cuda.device(table.device):
+        _check(load().sigtrain_embed_fwd(_ptr(tokens), _ptr(table), _ptr(out), tokens.numel(), V, D, scale, it, dt, _stream()))
+    return out
+
+
+def embed_bwd(tokens, grad_out, V, scale=1.0, grad_table=None, ws=None):
+    """dF/dtable [V, D] for upstream gradients grad_out[..., D]: the rows of every symbol summed in a fixed order."""
+    _dev(tokens, "tokens"); _dev(grad_out, "grad_out")
+    _together(grad_out, tokens, grad_table, ws)
+    D = grad_out.shape[-1] if grad_out.dim() else 0
+    if tuple(grad_out.shape) != (*tokens.shape, D):
+        raise ValueError("grad_out must be [*tokens.shape, D], got %s and %s" % (tuple(tokens.shape), tuple(grad_out.shape)))
+    dt, it = _st_dt(grad_out), _st_it(tokens)
+    if grad_table is None:
+        grad_table = torch.empty((V, D), dtype=grad_out.dtype, device=grad_out.device)
+    elif tuple(_dev(grad_table, "grad_table").shape) != (V, D) or grad_table.dtype != grad_out.dtype:
+        raise ValueError("grad_table must be %s of %s" % ((V, D), grad_out.dtype))
+    n = tokens.numel()
+    with torch.cuda.device(grad_out.device):
+        if ws is None:
+            ws = _scratch(load().sigtrain_embed_bwd_workspace_bytes(n, V, D, dt), grad_out.device)
+        _check(load().sigtrain_embed_bwd(_ptr(tokens), _ptr(grad_out), _ptr(grad_table), n, V, D, scale, it, dt, _ptr(ws), ws.numel(),
+                                         _stream()))
+    return grad_table
+
+
+def _entropy_shapes(h, w, targets, reduction):
+    _dev(h, "h"); _dev(w, "w"); _dev(targets, "targets")
+    _together(h, w, targets)
+    if h.dim() != 2 or w.dim() != 2 or h.shape[1] != w.shape[1] or tuple(targets.shape) != (h.shape[0],):
+        raise ValueError("h[T, D], w[V, D] and targets[T] expected, got %s, %s and %s" % (tuple(h.shape), tuple(w.shape), tuple(targets.shape)))
+    if h.dtype != w.dtype:
+        raise TypeError("h and w have different types: %s and %s" % (h.dtype, w.dtype))
+    if reduction not in _ST_REDUCTIONS:
+        raise ValueError("reduction must be none, mean or sum, got %r" % (reduction,))
+    return h.shape[0], w.shape[0], h.shape[1], _ST_REDUCTIONS[reduction], _st_it(targets), _st_dt(h)
+
+
+def entropy_fwd(h, w, targets, reduction="mean", ws=None):
+    """Softmax cross entropy of the read-out z = h w^T, h[T, D], w[V, D], targets[T] (outside 0 .. V - 1: no target).
+    Returns (loss [T] or [], lse[T], rows[1]): float32 (float64 for float64 arrays), rows with a target as a float64."""
+    T, V, D, red, it, dt = _entropy_shapes(h, w, targets, reduction)
+    acc = torch.float64 if dt == ST_F64 else torch.float32
+    loss = torch.empty((T,) if red == ST_NONE else (), dtype=acc, device=h.device)
+    lse = torch.empty((T,), dtype=acc, device=h.device)
+    rows = torch.empty((1,), dtype=torch.float64, device=h.device)
+    size = load().sigtrain_entropy_workspace_bytes
+    with torch.cuda.device(h.device):
+        if ws is None:
+            ws = _scratch(size(0, T, V, D, dt, 0), h.device, lambda: size(0, T, V, D, dt, 1))
+        _check(load().sigtrain_entropy_fwd(_ptr(h), _ptr(w), _ptr(targets), _ptr(loss), _ptr(lse), _ptr(rows), T, V, D, red, it, dt, _ptr(ws),
+                                           ws.numel(), _stream()))
+    return loss, lse, rows
+
+
+def entropy_bwd(h, w, targets, lse, rows, grad, reduction="mean", want_h=True, want_w=True, ws=None):
+    """(grad_h or None, grad_w or None) for the upstream gradient of entropy_fwd's loss; lse and rows are that call's."""
+    T, V, D, red, it, dt = _entropy_shapes(h, w, targets, reduction)
+    acc = torch.float64 if dt == ST_F64 else torch.float32
+    for name, t, shape, dtype in (("lse", lse, (T,), acc), ("rows", rows, (1,), torch.float64), ("grad", grad, (T,) if red == ST_NONE else (), acc)):
+        _dev(t, name)
+        _together(h, t)
+        if tuple(t.shape) != shape or t.dtype != dtype:
+            raise ValueError("%s must be %s of %s, got %s of %s" % (name, shape, dtype, tuple(t.shape), t.dtype))
+    gh = torch.empty_like(h) if want_h else None
+    gw = torch.empty_like(w) if want_w else None
+    size = load().sigtrain_entropy_workspace_bytes
+    with torch.cuda.device(h.device):
+        if ws is None:
+            ws = _scratch(size(1, T, V, D, dt, 0), h.device, lambda: size(1, T, V, D, dt, 1))
+        _check(load().sigtrain_entropy_bwd(_ptr(h), _ptr(w), _ptr(targets), _ptr(lse), _ptr(rows), _ptr(grad), _ptr(gh), _ptr(gw), T, V, D, red,
+                                           it, dt, _ptr(ws), ws.numel(), _stream()))
+    return gh, gw
+
+
+def _list(grads):
+    grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
+    for g in grads:
+        if not g.is_cuda:
+            raise ValueError("device tensors expected, got one on %s" % g.device)
+        _together(grads[0], g)
+    return grads
+
+
+def _tables(ts):
+    n = len(ts)
+    return (C.c_void_p * n)(*[t.data_ptr() for t in ts]), (C.c_int * n)(*[_st_dt(t) for t in ts])
+
+
+def _norm_device(grads):
+    return grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
+
+
+def grad_norm(grads):
+    """The Euclidean norm of all entries of a tensor or of several (contiguous device tensors of any floating types), as a float64 [] on the device."""
+    grads = _list(grads)
+    for g in grads:
+        _dev(g, "grads")
+    device, n = _norm_device(grads), len(grads)
+    norm = torch.empty((), dtype=torch.float64, device=device)
+    at, dts = _tables(grads)
+    counts = (C.c_int64 * n)(*[g.numel() for g in grads])
+    with torch.cuda.device(device):
+        ws = _scratch(load().sigtrain_clip_workspace_bytes(n), device)
+        _check(load().sigtrain_grad_norm(at, counts, dts, n, _ptr(norm), _ptr(ws), ws.numel(), _stream()))
+    return norm
+
+
+def clip(grads, max_norm, out=None):
+    """out[i] = grads[i] * min(1, max_norm / norm of all), in place for out = None; returns the norm, a float64 [] on the device.  Contiguous device
+    tensors; an output that is not its input must not overlap any of them."""
+    grads = _list(grads)
+    outs = grads if out is None else _list(out)
+    if len(outs) != len(grads):
+        raise ValueError("%d tensors, %d outputs" % (len(grads), len(outs)))
+    for g, o in zip(grads, outs):
+        _dev(g, "grads"); _dev(o, "out")
+        _together(g, o)
+        if g.shape != o.shape:
+            raise ValueError("an output of shape %s for a tensor of shape %s" % (tuple(o.shape), tuple(g.shape)))
+    device, n = _norm_device(grads), len(grads)
+    norm = torch.empty((), dtype=torch.float64, device=device)
+    at, dts = _tables(grads)
+    to, out_dts = (at, dts) if out is None else _tables(outs)
+    counts = (C.c_int64 * n)(*[g.numel() for g in grads])
+    with torch.cuda.device(device):
+        ws = _scratch(load().sigtrain_clip_workspace_bytes(n), device)
+        _check(load().sigtrain_clip(at, to, counts, dts, out_dts, n, max_norm, _ptr(norm), _ptr(ws), ws.numel(), _stream()))
+    return norm

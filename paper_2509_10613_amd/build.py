@@ -14,6 +14,10 @@ NATIVE = os.path.join(HERE, "_native.so")   # the autograd wrappers' host path (
 SOURCES = ["sk_api.hip", "sk_kernels.hip", "sk_lockstep.hip", "sk_solo.hip", "sk_solo_one.hip", "sk_tile.hip", "sk_tile_bwd.hip", "sk_quad.hip", "sk_four.hip", "sk_band.hip", "sk_wide.hip", "sk_split_lock.hip", "sk_split_band.hip", "sk_split_seg.hip", "sg_horner.hip", "sg_horner_bwd.hip", "sg_horner_bwd_matrix.hip", "sg_pieces.hip"]
 HEADERS = ["sk_plan.h", "sk_band.h", "sk_kernels.h", "sk_dev.h", "sk_lane.h", "sk_solo_impl.h", "sk_tile.h", "sk_quad.h", "sg_plan.h", "sg_kernels.h", "sg_dev.h"]
 PUBLIC = ["sigkernel.h", "signature.h"]
+# The operators of sigtrain.h: sources and headers of their own, so that a change to either half leaves the other's objects alone.
+TRAIN_SOURCES = ["st_api.hip", "st_embed.hip", "st_entropy.hip", "st_clip.hip"]
+TRAIN_HEADERS = ["st_kernels.h", "st_dev.h", "sk_error.h"]
+TRAIN_PUBLIC = ["sigkernel.h", "sigtrain.h"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -41,9 +45,16 @@ def _build_native():
         raise RuntimeError("g++ failed on sk_torch.cpp:\n" + r.stderr)
 
 
+def _headers_of(src):
+    mine, public = (TRAIN_HEADERS, TRAIN_PUBLIC) if src in TRAIN_SOURCES else (HEADERS, PUBLIC)
+    extra = ["sk_error.h"] if src == "sk_api.hip" else []
+    return [os.path.join(CSRC, f) for f in mine + extra] + [os.path.join(ROOT, "include", h) for h in public]
+
+
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.join(ROOT, "include", h) for h in PUBLIC]
-    native_deps = [os.path.join(CSRC, "sk_torch.cpp")] + [os.path.join(ROOT, "include", h) for h in PUBLIC]
+    sources = SOURCES + TRAIN_SOURCES
+    deps = [os.path.join(CSRC, f) for f in sources] + [h for f in sources for h in _headers_of(f)]
+    native_deps = [os.path.join(CSRC, "sk_torch.cpp")] + [os.path.join(ROOT, "include", h) for h in PUBLIC + TRAIN_PUBLIC]
     if not force and not _stale(LIB, deps):
         if _stale(NATIVE, native_deps):
             _build_native()
@@ -51,11 +62,9 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
 
-    hdrs = [os.path.join(CSRC, f) for f in HEADERS] + [os.path.join(ROOT, "include", h) for h in PUBLIC]
-
     def compile_one(src):
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
-        if not force and not extra_flags and not _stale(obj, [os.path.join(CSRC, src)] + hdrs):
+        if not force and not extra_flags and not _stale(obj, [os.path.join(CSRC, src)] + _headers_of(src)):
             return obj   # this object is newer than its source and every header
         cmd = ["hipcc"] + FLAGS + FILE_FLAGS.get(src, []) + list(extra_flags) + ["-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
@@ -67,7 +76,7 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         return obj
 
     with ThreadPoolExecutor(max_workers=8) as ex:
-        objs = list(ex.map(compile_one, SOURCES))
+        objs = list(ex.map(compile_one, sources))
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

@@ -13,6 +13,7 @@
 #include "sigkernel.h"
 #include "signature.h"
 #include "sg_kernels.h"
+#include "sk_error.h"
 #include "sk_kernels.h"
 
 namespace {
@@ -509,6 +510,8 @@ int dispatch(bool backward, bool gram, const void* x, const void* y, void* k, co
 }
 
 }  // namespace
+
+int sk::set_error(int code, const char* message) { return fail(code, "%s", message); }
 
 extern "C" {
 
