@@ -20,6 +20,10 @@ using f64x4 = __attribute__((ext_vector_type(4))) double;
 using bf16x8 = __attribute__((ext_vector_type(8))) bf16;
 using f16x8 = __attribute__((ext_vector_type(8))) f16;
 
+// c[j] += a b[j]^T.  Sums of float stay in the accumulation registers for as long as the products last: the instructions are written out, since the
+// compiler, left to place 256 sums and the operands of two steps, moves hundreds of registers between the two files in every step (128 x 128
+// classes and rows per wave: 960 against 1290 TFLOP/s).  What the compiler would wait for, `settle` does; operands come from
+// LDS, whose loads it waits for as for any instruction's.
 template <typename T>
 struct Types;
 template <>
@@ -27,25 +31,37 @@ struct Types<bf16> {
     using Sum = float;
     using Frag = bf16x8;   // 16 bytes of a row
     using Acc = f32x4;     // a lane's part of a 16 x 16 tile
-    static __device__ __forceinline__ Acc product(Frag a, Frag b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    template <int N>
+    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N])
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a), "v"(b[j]));
+    }
 };
 template <>
 struct Types<f16> {
     using Sum = float;
     using Frag = f16x8;
     using Acc = f32x4;
-    static __device__ __forceinline__ Acc product(Frag a, Frag b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    template <int N>
+    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N])
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a), "v"(b[j]));
+    }
 };
 template <>
 struct Types<float> {
     using Sum = float;
     using Frag = f32x4;
     using Acc = f32x4;
-    static __device__ __forceinline__ Acc product(Frag a, Frag b, Acc c)
+    template <int N>
+    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N])
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-        return c;
+        for (int k = 0; k < 4; ++k)   // (instructions on one sum lie apart)
+#pragma unroll
+            for (int j = 0; j < N; ++j) asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a[k]), "v"(b[j][k]));
     }
 };
 template <>
@@ -53,13 +69,31 @@ struct Types<double> {
     using Sum = double;
     using Frag = __attribute__((ext_vector_type(2))) double;
     using Acc = f64x4;
-    static __device__ __forceinline__ Acc product(Frag a, Frag b, Acc c)
+    template <int N>
+    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N])
     {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) c = __builtin_amdgcn_mfma_f64_16x16x4f64(a[i], b[i], c, 0, 0, 0);
-        return c;
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int j = 0; j < N; ++j) c[j] = __builtin_amdgcn_mfma_f64_16x16x4f64(a[k], b[j][k], c[j], 0, 0, 0);
     }
 };
+// Between instructions that write sums and instructions of other kinds that read or wrote them: more than the 19 cycles the longest of these
+// matrix instructions' results take.
+template <int M, int N>
+__device__ __forceinline__ void settle(f32x4 (&acc)[M][N])
+{
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (i + j == 0) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[i][j]));
+            else asm volatile("" : "+a"(acc[i][j]));
+}
+template <int M, int N>
+__device__ __forceinline__ void settle(f64x4 (&)[M][N])
+{
+}
 // The row of a 16 x 16 result tile that a lane's r-th number belongs to (its column is lane % 16).
 template <typename T>
 __device__ __forceinline__ int acc_row(int lane, int r)
@@ -88,7 +122,7 @@ __device__ __forceinline__ S exp_below(S x, S m)
 }
 
 // ------------------------------------------------------------------------------------------------ the products
-constexpr int kThreads = 256, kTile = kTileRows, kWaveTile = 64, kSub = kWaveTile / 16;
+constexpr int kThreads = 256;   // four waves, two by two
 
 struct Operands {
     const char *a, *b;
@@ -97,100 +131,192 @@ struct Operands {
     int64_t steps;              // of kStepBytes along k
 };
 
-template <typename T>
-using AccTile = typename Types<T>::Acc[kSub][kSub];
-
-// One workgroup's 128 x 128 tile: four waves of 64 x 64.  acc[i][j]: 16 x 16 tile of rows m0 + i * 16, columns n0 + j * 16.
-template <typename T>
-__device__ __forceinline__ void multiply(const Operands& o, int64_t m0, int64_t n0, AccTile<T>& acc, char* lds)
-{
+// A wave's tile is SUB x SUB tiles of 16 x 16, a workgroup's twice that on either side.  Large tiles read least from LDS per product: 128 x 128
+// per wave (256 x 256 per workgroup) take 1024 of the 2048 cycles a step's matrix instructions last, and 512 for the loads that arrive.  That is
+// 256 registers of sums (float; double sums take twice as many, so half the tile on either side).
+template <typename T, int SUB>
+struct Product {
     using Frag = typename Types<T>::Frag;
-    constexpr int kLoads = kTile * kStepBytes / 16 / kThreads;   // 16-byte chunks per thread and side
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w >> 1, wn = w & 1;
-#pragma unroll
-    for (int i = 0; i < kSub; ++i)
-#pragma unroll
-        for (int j = 0; j < kSub; ++j) acc[i][j] = {0, 0, 0, 0};
-    f32x4 ra[kLoads], rb[kLoads];
-    const char *pa[kLoads], *pb[kLoads];
-    int to[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int chunk = threadIdx.x + i * kThreads, row = chunk >> 3, c = chunk & 7;
-        // rows behind the last are read from the last: their results are dropped
-        pa[i] = o.a + (m0 + row < o.m ? m0 + row : o.m - 1) * o.a_pitch + c * 16;
-        pb[i] = o.b + (n0 + row < o.n ? n0 + row : o.n - 1) * o.b_pitch + c * 16;
-        to[i] = row * kStepBytes + ((c ^ (row & 7)) << 4);   // (the chunks of eight rows' same columns lie in different banks)
+    using Acc = typename Types<T>::Acc;
+    static constexpr int kWave = SUB * 16, kTile = 2 * kWave;
+    static constexpr int kSide = kTile * kStepBytes;           // bytes of one operand's step in LDS
+    static constexpr size_t kLds = 4 * kSide;                  // two steps of two operands
+    static constexpr int kLoads = kSide / (16 * kThreads);     // 16-byte loads per thread, side and step
+
+    Acc acc[SUB][SUB];
+    int lane, wm, wn;
+
+    // 64 lanes' 16 bytes to LDS address `to` and behind it, past the registers.  Not counted by the compiler, which would wait for all of
+    // them before any read of LDS: the waits below are the kernel's own.  (m0 is left as it was.)
+    static __device__ __forceinline__ void load(const char* from, uint32_t to)
+    {
+        uint32_t kept;
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+                     : "=&s"(kept)
+                     : "s"(to), "v"(from)
+                     : "memory");
     }
+
+    // The tile with rows m0.. of A and n0.. of B.  A step's operands lie in LDS as rows of 128 bytes, the 16-byte chunks of a row exchanged by
+    // its number modulo 8, so that eight rows' chunks of one column lie in different banks.  Two steps are under way: a wave reads the second half
+    // of step s, multiplies the first half, and after the one barrier of a step (everybody has read step s, step s + 1 has arrived) sends for
+    // step s + 2, reads the first half of step s + 1 and multiplies the second half of step s.
+    __device__ __forceinline__ void run(const Operands& o, int64_t m0, int64_t n0, char* lds)
+    {
+        lane = threadIdx.x & 63;
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wm = w >> 1;
+        wn = w & 1;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        ra[i] = *reinterpret_cast<const f32x4*>(pa[i]);
-        rb[i] = *reinterpret_cast<const f32x4*>(pb[i]);
-    }
-    for (int64_t s = 0; s < o.steps; ++s) {
-        char* la = lds + (s & 1) * (2 * kTile * kStepBytes);
-        char* lb = la + kTile * kStepBytes;
+        for (int i = 0; i < SUB; ++i)
+#pragma unroll
+            for (int j = 0; j < SUB; ++j) acc[i][j] = {0, 0, 0, 0};
+        const char *pa[kLoads], *pb[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            *reinterpret_cast<f32x4*>(la + to[i]) = ra[i];
-            *reinterpret_cast<f32x4*>(lb + to[i]) = rb[i];
+            // (rows behind the last are read from the last: their results are dropped)
+            const int row = (i * 4 + w) * 8 + (lane >> 3), c = ((lane & 7) ^ (row & 7)) * 16;
+            pa[i] = o.a + (m0 + row < o.m ? m0 + row : o.m - 1) * o.a_pitch + c;
+            pb[i] = o.b + (n0 + row < o.n ? n0 + row : o.n - 1) * o.b_pitch + c;
         }
-        __syncthreads();
-        if (s + 1 < o.steps)
+        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+        auto send_one = [&](int half, int i) {
+            load(pa[i], base + half * 2 * kSide + (i * 4 + w) * 1024);
+            load(pb[i], base + half * 2 * kSide + kSide + (i * 4 + w) * 1024);
+            pa[i] += kStepBytes;
+            pb[i] += kStepBytes;
+        };
+        auto send = [&](int half) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                ra[i] = *reinterpret_cast<const f32x4*>(pa[i] + (s + 1) * kStepBytes);
-                rb[i] = *reinterpret_cast<const f32x4*>(pb[i] + (s + 1) * kStepBytes);
+            for (int i = 0; i < kLoads; ++i) send_one(half, i);
+        };
+        settle(acc);
+        Frag fa[2][SUB], fb[2][SUB];
+        const int at = (lane & 15) * kStepBytes + (((lane >> 4) ^ (lane & 7)) << 4);
+        const char *la = lds + wm * kWave * kStepBytes + at, *lb = lds + kSide + wn * kWave * kStepBytes + at;
+        // the i-th part of a half step's operands (the second half's chunks are four further on: bit 6 of the address, exchanged or not)
+        auto read = [&](int half, int kk, int i) {
+            const int to = half * 2 * kSide + i * 16 * kStepBytes;
+            fb[kk][i] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(lb - lds) ^ 64) + to : lb + to);
+            fa[kk][i] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(la - lds) ^ 64) + to : la + to);
+        };
+        // step s in one half of the LDS, s + 1 in the other; more: there is a step s + 2.  What is read and sent for is strewn among the
+        // products of the row before, in the order written.
+        auto step = [&](int half, auto next, auto more) {
+#pragma unroll
+            for (int i = 0; i < SUB; ++i) {
+                if (i < SUB / 2) {
+                    read(half, 1, 2 * i);
+                    read(half, 1, 2 * i + 1);
+                }
+                Types<T>::products(fa[0][i], fb[0], acc[i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (decltype(next)::value) {
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+                __builtin_amdgcn_s_barrier();
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            Frag fa[kSub], fb[kSub];
+            for (int i = 0; i < SUB; ++i) {
+                if constexpr (decltype(next)::value)
+                    if (i < SUB / 2) {
+                        read(half ^ 1, 0, 2 * i);
+                        read(half ^ 1, 0, 2 * i + 1);
+                    }
+                if constexpr (decltype(more)::value)
+                    if (i >= SUB / 2)
 #pragma unroll
-            for (int i = 0; i < kSub; ++i) {
-                const int c = ((kk * 4 + (lane >> 4)) ^ (lane & 7)) << 4;
-                fa[i] = *reinterpret_cast<const Frag*>(la + (wm * kWaveTile + i * 16 + (lane & 15)) * kStepBytes + c);
-                fb[i] = *reinterpret_cast<const Frag*>(lb + (wn * kWaveTile + i * 16 + (lane & 15)) * kStepBytes + c);
+                        for (int l = 0; l < 2 * kLoads / SUB; ++l) send_one(half, (i - SUB / 2) * (2 * kLoads / SUB) + l);
+                Types<T>::products(fa[1][i], fb[1], acc[i]);
+                __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int i = 0; i < kSub; ++i)
-#pragma unroll
-                for (int j = 0; j < kSub; ++j) acc[i][j] = Types<T>::product(fa[i], fb[j], acc[i][j]);
+        };
+        send(0);
+        if (o.steps > 1) {
+            send(1);
+            asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * kLoads) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         }
-        // (the next step writes the other half; a wave reaches that write of the step after next only past the next barrier)
+        __builtin_amdgcn_s_barrier();
+#pragma unroll
+        for (int i = 0; i < SUB; ++i) read(0, 0, i);
+        int half = 0;
+        for (int64_t s = 2; s < o.steps; ++s) {
+            step(half, std::true_type{}, std::true_type{});
+            half ^= 1;
+        }
+        if (o.steps > 1) {
+            step(half, std::true_type{}, std::false_type{});
+            half ^= 1;
+        }
+        step(half, std::false_type{}, std::false_type{});
+        settle(acc);
+        __syncthreads();   // (what follows may use the LDS)
     }
+};
+// Which tile a workgroup takes.  Workgroups go to the eight dies in turn, and a die's 32 compute units share a cache: a die's
+// workgroups get tiles that are neighbours, eight by four.
+struct TileOrder {
+    int64_t tiles_m, tiles_n;
+};
+__device__ __forceinline__ void tile_of(const TileOrder& t, int64_t& m, int64_t& n)
+{
+    constexpr int64_t kDies = 8, kAcross = 4;
+    const int64_t all = t.tiles_m * t.tiles_n, die = blockIdx.x % kDies, each = all / kDies, more = all % kDies;
+    const int64_t at = die * each + (die < more ? die : more) + blockIdx.x / kDies;
+    const int64_t group = at / (t.tiles_m * kAcross), left = at - group * t.tiles_m * kAcross;
+    const int64_t across = t.tiles_n - group * kAcross < kAcross ? t.tiles_n - group * kAcross : kAcross;
+    m = left / across;
+    n = group * kAcross + left % across;
 }
-constexpr size_t kProductLds = 4 * kTile * kStepBytes;
 
 // Forward: every row's maximum and sum of exponentials over the tile's classes (A: classes of w, B: rows of h).
-template <typename T>
-__global__ __launch_bounds__(kThreads) void stats_kernel(Operands o, const void* targets, int it, int64_t first_class, int64_t V,
+template <typename T, int SUB>
+__global__ __launch_bounds__(kThreads, 1) void stats_kernel(Operands o, TileOrder order, const void* targets, int it, int64_t first_class, int64_t V,
                                                          typename Types<T>::Sum* part_max, typename Types<T>::Sum* part_sum,
                                                          typename Types<T>::Sum* hit)
 {
     using S = typename Types<T>::Sum;
-    __shared__ __align__(16) char lds[kProductLds];
-    const int64_t m0 = (int64_t)blockIdx.x * kTile, n0 = (int64_t)blockIdx.y * kTile;
-    AccTile<T> acc;
-    multiply<T>(o, m0, n0, acc, lds);
-    __syncthreads();
+    using P = Product<T, SUB>;
+    constexpr int kTile = P::kTile, kWave = P::kWave;
+    extern __shared__ __align__(16) char lds[];
+    int64_t tile_m, tile_n;
+    tile_of(order, tile_m, tile_n);
+    const int64_t m0 = tile_m * kTile, n0 = tile_n * kTile;
+    P p;
+    p.run(o, m0, n0, lds);
+    auto& acc = p.acc;
+    const int lane = p.lane, wm = p.wm, wn = p.wn;
     S* waves = reinterpret_cast<S*>(lds);   // [2 halves of the classes][2: maximum, sum][kTile]
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w >> 1, wn = w & 1;
+    if (m0 + kTile > o.m)   // classes behind the last
 #pragma unroll
-    for (int j = 0; j < kSub; ++j) {
-        const int64_t row = n0 + wn * kWaveTile + j * 16 + (lane & 15);
+        for (int i = 0; i < SUB; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (m0 + wm * kWave + i * 16 + acc_row<T>(lane, r) >= o.m)
+#pragma unroll
+                    for (int j = 0; j < SUB; ++j) acc[i][j][r] = lowest<S>();
+#pragma unroll
+    for (int j = 0; j < SUB; ++j) {
+        const int64_t row = n0 + wn * kWave + j * 16 + (lane & 15);
         const int64_t target = row < o.n ? load_index(targets, row, it) : -1;
-        const int64_t wanted = target >= 0 && target < V ? target - first_class - m0 - wm * kWaveTile : -1;
-        S top = lowest<S>();
+        const int64_t wanted64 = target >= 0 && target < V ? target - first_class - m0 - wm * kWave : -1;
+        const int wanted = wanted64 >= 0 && wanted64 < kWave ? (int)wanted64 : -1;   // of this wave's classes
+        S top = lowest<S>(), mine = 0;
+        bool found = false;
 #pragma unroll
-        for (int i = 0; i < kSub; ++i)
+        for (int i = 0; i < SUB; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int at = i * 16 + acc_row<T>(lane, r);
-                if (m0 + wm * kWaveTile + at >= o.m) acc[i][j][r] = lowest<S>();
-                else if (at == wanted) hit[row] = acc[i][j][r];
-                // (a maximum that a NaN passes through)
-                top = acc[i][j][r] > top || acc[i][j][r] != acc[i][j][r] ? acc[i][j][r] : top;
+                const S z = acc[i][j][r];
+                const bool here = i * 16 + acc_row<T>(lane, r) == wanted;
+                mine = here ? z : mine;
+                found |= here;
+                top = z > top || z != z ? z : top;   // (a maximum that a NaN passes through)
             }
+        if (found) hit[row] = mine;
 #pragma unroll
         for (int x = 16; x < 64; x *= 2) {
             const S other = __shfl_xor(top, x);
@@ -198,88 +324,139 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Operands o, const void*
         }
         S sum = 0;
 #pragma unroll
-        for (int i = 0; i < kSub; ++i)
+        for (int i = 0; i < SUB; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) sum += exp_below<T>(acc[i][j][r], top);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (lane < 16) {
-            waves[(wm * 2 + 0) * kTile + wn * kWaveTile + j * 16 + lane] = top;
-            waves[(wm * 2 + 1) * kTile + wn * kWaveTile + j * 16 + lane] = sum;
+            waves[(wm * 2 + 0) * kTile + wn * kWave + j * 16 + lane] = top;
+            waves[(wm * 2 + 1) * kTile + wn * kWave + j * 16 + lane] = sum;
         }
     }
     __syncthreads();
+    static_assert(kTile <= kThreads);
     const int64_t row = n0 + threadIdx.x;
     if (threadIdx.x < kTile && row < o.n) {
         const S a = waves[threadIdx.x], b = waves[2 * kTile + threadIdx.x];
         const S top = b > a || b != b ? b : a;
-        part_max[(int64_t)blockIdx.x * o.n + row] = top;
-        part_sum[(int64_t)blockIdx.x * o.n + row] =
+        part_max[tile_m * o.n + row] = top;
+        part_sum[tile_m * o.n + row] =
             waves[kTile + threadIdx.x] * exp_below<T>(a, top) + waves[3 * kTile + threadIdx.x] * exp_below<T>(b, top);
     }
 }
 
 // Backward: the gradients of the piece's logits, g[row][class] and gt[class][row], zeros up to whole steps.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void grads_kernel(Operands o, const void* targets, int it, int64_t first_class,
+template <typename T, int SUB>
+__global__ __launch_bounds__(kThreads, 1) void grads_kernel(Operands o, TileOrder order, const void* targets, int it, int64_t first_class,
                                                          const typename Types<T>::Sum* lse, const typename Types<T>::Sum* up, T* g,
                                                          int64_t g_pitch, T* gt, int64_t gt_pitch)
 {
     using S = typename Types<T>::Sum;
-    __shared__ __align__(16) char lds[kProductLds];
-    const int64_t m0 = (int64_t)blockIdx.x * kTile, n0 = (int64_t)blockIdx.y * kTile;
-    AccTile<T> acc;
-    multiply<T>(o, m0, n0, acc, lds);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w >> 1, wn = w & 1;
+    using P = Product<T, SUB>;
+    constexpr int kTile = P::kTile, kWave = P::kWave;
+    extern __shared__ __align__(16) char lds[];
+    int64_t tile_m, tile_n;
+    tile_of(order, tile_m, tile_n);
+    const int64_t m0 = tile_m * kTile, n0 = tile_n * kTile;
+    P p;
+    p.run(o, m0, n0, lds);
+    auto& acc = p.acc;
+    const int lane = p.lane, wm = p.wm, wn = p.wn;
+    const bool inside = m0 + kTile <= o.m;
 #pragma unroll
-    for (int j = 0; j < kSub; ++j) {
-        const int64_t row = n0 + wn * kWaveTile + j * 16 + (lane & 15);
+    for (int j = 0; j < SUB; ++j) {
+        const int64_t row = n0 + wn * kWave + j * 16 + (lane & 15);
         const bool there = row < o.n;
         const int64_t target = there ? load_index(targets, row, it) : -1;
-        const int64_t wanted = target - first_class - m0 - wm * kWaveTile;
+        const int64_t wanted64 = target - first_class - m0 - wm * kWave;
+        const int wanted = wanted64 >= 0 && wanted64 < kWave ? (int)wanted64 : -1;
         const S u = there ? up[row] : (S)0, l = there ? lse[row] : (S)0;
 #pragma unroll
-        for (int i = 0; i < kSub; ++i)
+        for (int i = 0; i < SUB; ++i) {
+            const int64_t cls = m0 + wm * kWave + i * 16;
+            Vec<T, 4> v;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int at = i * 16 + acc_row<T>(lane, r);
-                const int64_t cls = m0 + wm * kWaveTile + at;
+                const int at = acc_row<T>(lane, r);
+                const S p = exp_of(acc[i][j][r] - l, T{}) - (i * 16 + at == wanted ? (S)1 : (S)0);
                 // rows without a target (u is 0) stay 0 whatever their logits are
-                const S p = exp_of(acc[i][j][r] - l, T{}) - (at == wanted ? (S)1 : (S)0);
-                const T v = (T)(u != 0 && cls < o.m ? u * p : (S)0);
-                if (there && cls < g_pitch) g[row * g_pitch + cls] = v;
-                if (cls < o.m && row < gt_pitch) gt[cls * gt_pitch + row] = v;
+                v.v[r] = (T)(u != 0 && (inside || cls + at < o.m) ? u * p : (S)0);
             }
+            if constexpr (sizeof(T) == 8) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (there && cls + acc_row<T>(lane, r) < g_pitch) g[row * g_pitch + cls + acc_row<T>(lane, r)] = v.v[r];
+            } else {
+                // (g_pitch is a multiple of 16: the tile is in or out)
+                if (there && cls < g_pitch) store_vec(g + row * g_pitch + cls + acc_row<T>(lane, 0), v);
+            }
+            if (row < gt_pitch)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (inside || cls + acc_row<T>(lane, r) < o.m) gt[(cls + acc_row<T>(lane, r)) * gt_pitch + row] = v.v[r];
+        }
     }
 }
 
-// out[n][m] (pitch D): the first piece's results set the sum, the last one's leave it rounded, divided by the gradients' scaling.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void product_kernel(Operands o, typename Types<T>::Sum* sum, T* out, int64_t D, bool first, bool last,
-                                                           const typename Types<T>::Sum* unscale)
+// out[n][m] (pitch D), divided by the gradients' scaling and rounded.  SUMS: over several pieces; the first sets `sum`, the last leaves the results.
+template <typename T, int SUB, bool SUMS>
+__global__ __launch_bounds__(kThreads, 1) void product_kernel(Operands o, TileOrder order, typename Types<T>::Sum* sum, T* out, int64_t D, bool first,
+                                                              bool last, const typename Types<T>::Sum* unscale)
 {
     using S = typename Types<T>::Sum;
-    __shared__ __align__(16) char lds[kProductLds];
-    const int64_t m0 = (int64_t)blockIdx.x * kTile, n0 = (int64_t)blockIdx.y * kTile;
-    AccTile<T> acc;
-    multiply<T>(o, m0, n0, acc, lds);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w >> 1, wn = w & 1;
+    using P = Product<T, SUB>;
+    constexpr int kTile = P::kTile, kWave = P::kWave;
+    extern __shared__ __align__(16) char lds[];
+    int64_t tile_m, tile_n;
+    tile_of(order, tile_m, tile_n);
+    const int64_t m0 = tile_m * kTile, n0 = tile_n * kTile;
+    P p;
+    p.run(o, m0, n0, lds);
+    auto& acc = p.acc;
+    const int lane = p.lane, wm = p.wm, wn = p.wn;
     const S f = *unscale;
+    // (rows without a target stay 0 whatever is upstream)
+    auto rounded = [&](S x) { return (T)(x == 0 ? x : x * f); };
 #pragma unroll
-    for (int j = 0; j < kSub; ++j) {
-        const int64_t n = n0 + wn * kWaveTile + j * 16 + (lane & 15);
+    for (int j = 0; j < SUB; ++j) {
+        const int64_t n = n0 + wn * kWave + j * 16 + (lane & 15);
         if (n >= o.n) continue;
 #pragma unroll
-        for (int i = 0; i < kSub; ++i)
+        for (int i = 0; i < SUB; ++i) {
+            const int64_t m = m0 + wm * kWave + i * 16 + acc_row<T>(lane, 0), at = n * D + m;
+            constexpr int kApart = sizeof(T) == 8 ? 4 : 1, kSpan = 3 * kApart;   // the lane's four numbers
+            Vec<S, 4> x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x.v[r] = acc[i][j][r];
+            if (kApart == 1 && m + kSpan < o.m) {
+                if constexpr (SUMS) {
+                    if (!first) {
+                        const Vec<S, 4> before = load_vec<S, 4>(sum + at);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x.v[r] += before.v[r];
+                    }
+                    if (!last) {
+                        store_vec(sum + at, x);
+                        continue;
+                    }
+                }
+                Vec<T, 4> v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v.v[r] = rounded(x.v[r]);
+                store_vec(out + at, v);
+                continue;
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int64_t m = m0 + wm * kWaveTile + i * 16 + acc_row<T>(lane, r);
-                if (m >= o.m) continue;
-                S x = acc[i][j][r];
-                if (!first) x += sum[n * D + m];
-                if (last) out[n * D + m] = (T)(x * f);
-                else sum[n * D + m] = x;
+                if (m + r * kApart >= o.m) continue;
+                const int64_t to = at + r * kApart;
+                S y = x.v[r];
+                if (SUMS && !first) y += sum[to];
+                if (SUMS && !last) sum[to] = y;
+                else out[to] = rounded(y);
             }
+        }
     }
 }
 
@@ -402,42 +579,43 @@ __global__ __launch_bounds__(1024) void reduce_kernel(const S* losses, const voi
     if (reduction == ST_MEAN) *loss = (S)(n > 0 ? sum / n : 0.0);
 }
 
-// Every row's upstream gradient, and scaling[0] = 1 / the factor it has been multiplied by: for f16 a power of two that takes the
-// largest to 2^13 .. 2^14 (the gradients of a mean over thousands of rows would otherwise be subnormal).  One workgroup.
+// Every row's upstream gradient over the largest of them, and that one: scaling[0].  The logits' gradients are rounded to T, and a common
+// factor that T does not hold (one over the number of rows) would put all of them off by the same part of a step.  f16 takes 2^14 times as
+// much, or small probabilities would be subnormal.  One workgroup.
 template <typename T>
 __global__ __launch_bounds__(1024) void upstream_kernel(const typename Types<T>::Sum* grad, const void* targets, int it, int64_t rows, int64_t V,
                                                         int reduction, const double* count, typename Types<T>::Sum* up,
                                                         typename Types<T>::Sum* scaling)
 {
     using S = typename Types<T>::Sum;
-    __shared__ float tops[16];
-    auto value = [&](int64_t i) {
+    constexpr S kRange = std::is_same_v<T, f16> ? (S)16384 : (S)1;
+    __shared__ S tops[16];
+    auto has = [&](int64_t i) {
         const int64_t t = load_index(targets, i, it);
-        if (t < 0 || t >= V) return (S)0;
-        if (reduction == ST_NONE) return grad[i];
-        return reduction == ST_SUM ? grad[0] : (S)((double)grad[0] / *count);
+        return t >= 0 && t < V;
     };
-    S factor = 1;
-    if constexpr (std::is_same_v<T, f16>) {
-        float top = 0;
-        for (int64_t i = threadIdx.x; i < rows; i += 1024) top = fmaxf(top, fabsf(value(i)));
+    S top = 1;
+    if (reduction == ST_NONE) {
+        top = 0;
+        for (int64_t i = threadIdx.x; i < rows; i += 1024) {
+            const S a = has(i) ? (grad[i] < 0 ? -grad[i] : grad[i]) : (S)0;
+            top = a > top ? a : top;
+        }
 #pragma unroll
-        for (int o = 32; o > 0; o /= 2) top = fmaxf(top, __shfl_xor(top, o));
+        for (int o = 32; o > 0; o /= 2) {
+            const S a = __shfl_xor(top, o);
+            top = a > top ? a : top;
+        }
         if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
         __syncthreads();
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, tops[i]);
-        int e = 0;
-        if (top > 0 && top <= 3.4028234e38f) {
-            frexpf(top, &e);
-            e = 14 - e;
-            e = e > 126 ? 126 : e < -126 ? -126 : e;
-        }
-        factor = ldexpf(1.0f, e);
-        if (threadIdx.x == 0) *scaling = ldexpf(1.0f, -e);
-    } else {
-        if (threadIdx.x == 0) *scaling = 1;
+        for (int i = 0; i < 16; ++i) top = tops[i] > top ? tops[i] : top;
+        if (!(top > 0 && top < (S)__builtin_inf())) top = 1;
     }
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) up[i] = value(i) * factor;
+    for (int64_t i = threadIdx.x; i < rows; i += 1024) up[i] = !has(i) ? (S)0 : reduction == ST_NONE ? grad[i] / top * kRange : kRange;
+    if (threadIdx.x == 0) {
+        const S all = reduction == ST_MEAN ? (S)((double)grad[0] / *count) : reduction == ST_SUM ? grad[0] : top;
+        *scaling = all / kRange;
+    }
 }
 
 unsigned blocks_for(int64_t items) { return (unsigned)((items + 255) / 256 < 16384 ? (items + 255) / 256 : 16384); }
@@ -466,7 +644,25 @@ Operands operands(const T* a, int64_t a_cols, int64_t m, const T* b, int64_t b_c
     return {reinterpret_cast<const char*>(a), reinterpret_cast<const char*>(b), a_cols * (int64_t)sizeof(T), b_cols * (int64_t)sizeof(T), m, n,
             k * (int64_t)sizeof(T) / kStepBytes};
 }
-dim3 tiles_of(int64_t m, int64_t n) { return dim3((unsigned)((m + kTile - 1) / kTile), (unsigned)((n + kTile - 1) / kTile)); }
+template <typename T>
+constexpr int kSub = sizeof(T) == 8 ? 4 : 8;
+template <typename T>
+TileOrder tiles_of(int64_t m, int64_t n)
+{
+    constexpr int kTile = Product<T, kSub<T>>::kTile;
+    static_assert(kTile >= kTileLeast && kTileRows % kTile == 0);
+    return {(m + kTile - 1) / kTile, (n + kTile - 1) / kTile};
+}
+// (more than 64 KiB of LDS have to be asked for, once per device)
+template <typename T, typename K, typename... Args>
+hipError_t launch_product(K kernel, const TileOrder& t, hipStream_t st, const Args&... args)
+{
+    constexpr size_t lds = Product<T, kSub<T>>::kLds;
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+    kernel<<<(unsigned)(t.tiles_m * t.tiles_n), kThreads, lds, st>>>(args...);
+    return hipGetLastError();
+}
 
 template <typename T>
 hipError_t run_fwd(const EntropyPlan& p, const T* h, const T* w, const void* targets, void* loss, void* lse, double* rows, int reduction, int it,
@@ -481,7 +677,7 @@ hipError_t run_fwd(const EntropyPlan& p, const T* h, const T* w, const void* tar
     hipError_t e = in_steps(h, p.T, p.D, p.Dp, ws + p.off_h, &hs, st);
     if (e != hipSuccess) return e;
     S *run_max = reinterpret_cast<S*>(ws + p.off_max), *run_sum = reinterpret_cast<S*>(ws + p.off_sum), *hit = reinterpret_cast<S*>(ws + p.off_hit);
-    const int64_t most = p.piece / kTile;
+    const int64_t most = p.piece / kTileLeast;
     S *part_max = reinterpret_cast<S*>(ws + p.off_part), *part_sum = part_max + most * p.T;
     // (the running maxima are dead where the losses of the rows are written: a thread reads its own first)
     S* losses = reduction == ST_NONE ? static_cast<S*>(loss) : run_max;
@@ -490,9 +686,9 @@ hipError_t run_fwd(const EntropyPlan& p, const T* h, const T* w, const void* tar
         const T* wsrc;
         if ((e = in_steps(w + first * p.D, n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
         const Operands o = operands(wsrc, p.Dp, n, hs, p.Dp, p.T, p.Dp);
-        const dim3 grid = tiles_of(n, p.T);
-        ST_TRY((stats_kernel<T><<<grid, kThreads, 0, st>>>(o, targets, it, first, p.V, part_max, part_sum, hit)));
-        ST_TRY((join_kernel<T><<<(unsigned)((p.T + 63) / 64), 1024, 0, st>>>(part_max, part_sum, grid.x, p.T, i == 0, i + 1 == p.pieces, run_max,
+        const TileOrder t = tiles_of<T>(n, p.T);
+        if ((e = launch_product<T>(stats_kernel<T, kSub<T>>, t, st, o, t, targets, it, first, p.V, part_max, part_sum, hit)) != hipSuccess) return e;
+        ST_TRY((join_kernel<T><<<(unsigned)((p.T + 63) / 64), 1024, 0, st>>>(part_max, part_sum, t.tiles_m, p.T, i == 0, i + 1 == p.pieces, run_max,
                                                                             run_sum, hit, targets, it, p.V, static_cast<S*>(lse), losses)));
     }
     ST_TRY((reduce_kernel<S><<<1, 1024, 0, st>>>(losses, targets, it, p.T, p.V, reduction, static_cast<S*>(loss), rows)));
@@ -527,15 +723,22 @@ hipError_t run_bwd(const EntropyPlan& p, const T* h, const T* w, const void* tar
         const T* wsrc;
         if ((e = in_steps(w + first * p.D, n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
         const Operands logits = operands(wsrc, p.Dp, n, hs, p.Dp, p.T, p.Dp);
-        ST_TRY((grads_kernel<T><<<tiles_of(n, p.T), kThreads, 0, st>>>(logits, targets, it, first, static_cast<const S*>(lse), up, g, np, gt, p.Tp)));
+        TileOrder t = tiles_of<T>(n, p.T);
+        if ((e = launch_product<T>(grads_kernel<T, kSub<T>>, t, st, logits, t, targets, it, first, static_cast<const S*>(lse), up, g, np, gt, p.Tp)) !=
+            hipSuccess)
+            return e;
         if (grad_h) {
             if ((e = turn(w + first * p.D, wt, n, np, nullptr)) != hipSuccess) return e;
             const Operands o = operands(wt, np, p.D, g, np, p.T, np);
-            ST_TRY((product_kernel<T><<<tiles_of(p.D, p.T), kThreads, 0, st>>>(o, dh, grad_h, p.D, i == 0, i + 1 == p.pieces, scaling)));
+            t = tiles_of<T>(p.D, p.T);
+            if ((e = launch_product<T>(p.pieces > 1 ? product_kernel<T, kSub<T>, true> : product_kernel<T, kSub<T>, false>, t, st, o, t, dh, grad_h, p.D, i == 0,
+                                       i + 1 == p.pieces, scaling)) != hipSuccess) return e;
         }
         if (grad_w) {
             const Operands o = operands(ht, p.Tp, p.D, gt, p.Tp, n, p.Tp);
-            ST_TRY((product_kernel<T><<<tiles_of(p.D, n), kThreads, 0, st>>>(o, nullptr, grad_w + first * p.D, p.D, true, true, scaling)));
+            t = tiles_of<T>(p.D, n);
+            if ((e = launch_product<T>(product_kernel<T, kSub<T>, false>, t, st, o, t, (S*)nullptr, grad_w + first * p.D, p.D, true, true, scaling)) != hipSuccess)
+                return e;
         }
     }
     return hipSuccess;
@@ -581,7 +784,7 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
             p.off_max = take(T, p.sum_size);
             p.off_sum = take(T, p.sum_size);
             p.off_hit = take(T, p.sum_size);
-            p.off_part = take(2 * T * (piece / kTile), p.sum_size);
+            p.off_part = take(2 * T * (piece / kTileLeast), p.sum_size);
         } else {
             p.off_up = take(T + 2, p.sum_size);
             p.off_ht = take(D * p.Tp, p.size);
@@ -592,20 +795,20 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
         }
         p.total = at;
     };
-    const int64_t all = (V + kTile - 1) / kTile * kTile;
+    const int64_t all = (V + kTileRows - 1) / kTileRows * kTileRows;
     if (least) {
-        lay(kTile);
+        lay(kTileRows);
         return p;
     }
     // Pieces as large as 512 MiB of what a class takes: the fewer there are, the less often the sums of grad_h are read and written.
-    const int64_t each = backward ? 2 * p.Tp * p.size + 2 * p.Dp * p.size : p.Dp * p.size + 2 * T * p.sum_size / kTile + 1;
-    int64_t most = ((int64_t)512 << 20) / each / kTile * kTile;
-    if (most < kTile) most = kTile;
+    const int64_t each = backward ? 2 * p.Tp * p.size + 2 * p.Dp * p.size : p.Dp * p.size + 2 * T * p.sum_size / kTileLeast + 1;
+    int64_t most = ((int64_t)512 << 20) / each / kTileRows * kTileRows;
+    if (most < kTileRows) most = kTileRows;
     if (most > ((int64_t)1 << 22)) most = (int64_t)1 << 22;   // (tiles of a piece are a grid's second index)
     for (int64_t count = (all + most - 1) / most;; ++count) {
-        const int64_t piece = ((all + count - 1) / count + kTile - 1) / kTile * kTile;
+        const int64_t piece = ((all + count - 1) / count + kTileRows - 1) / kTileRows * kTileRows;
         lay(piece);
-        if (ws_bytes == 0 || p.total <= ws_bytes || piece == kTile) return p;
+        if (ws_bytes == 0 || p.total <= ws_bytes || piece == kTileRows) return p;
     }
 }
 

@@ -35,7 +35,8 @@ hipError_t embed_bwd(const EmbedPlan& p, const void* tokens, const void* grad_ou
 // One call's pieces of the classes and scratch.  Everything that is multiplied has rows of whole steps (kStepBytes), zeros behind the last entry:
 // the caller's arrays where they have that form, copies elsewhere.
 constexpr int kStepBytes = 128;   // of a row, taken at a time by the products
-constexpr int kTileRows = 128;    // classes and rows per workgroup of the products
+constexpr int kTileRows = 256;    // pieces of the classes are multiples of this
+constexpr int kTileLeast = 128;   // classes and rows per workgroup of the products: this or twice as many
 struct EntropyPlan {
     int64_t T, V, D;
     int size, sum_size;        // bytes of an element and of a sum
