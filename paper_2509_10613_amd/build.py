@@ -23,7 +23,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-ato
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 # Per source file.  The tile backward kernel moves every MFMA result on (to LDS, to atomics): with the results in
 # vector registers instead of accumulation registers the copies between the two fall away (c5 backward: -1 %).
-FILE_FLAGS = {"sk_tile_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# st_entropy.hip says that its loads to LDS change m0, which the compiler keeps nothing in and warns of.
+FILE_FLAGS = {"sk_tile_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "st_entropy.hip": ["-Wno-inline-asm"]}
 
 
 def _stale(target, deps):

@@ -9,6 +9,8 @@
 // every type: a lane holds 16 consecutive bytes of a row, which are one matrix instruction's operand for 16-bit types and four or two
 // instructions' for float and double (the order of k does not matter as long as both sides have the same).  The side whose index the
 // result's rows run along is B: a lane then holds results that lie side by side in a row.
+#include <utility>
+
 #include "st_dev.h"
 #include "st_kernels.h"
 
@@ -20,7 +22,7 @@ using f64x4 = __attribute__((ext_vector_type(4))) double;
 using bf16x8 = __attribute__((ext_vector_type(8))) bf16;
 using f16x8 = __attribute__((ext_vector_type(8))) f16;
 
-// c[j] += a b[j]^T.  Sums of float stay in the accumulation registers for as long as the products last: the instructions are written out, since the
+// c[j] += a b[j]^T; between(j) after the j-th: the other instructions that hide behind the matrix instructions.  Sums of float stay in the accumulation registers for as long as the products last: the instructions are written out, since the
 // compiler, left to place 256 sums and the operands of two steps, moves hundreds of registers between the two files in every step (128 x 128
 // classes and rows per wave: 960 against 1290 TFLOP/s).  What the compiler would wait for, `settle` does; operands come from
 // LDS, whose loads it waits for as for any instruction's.
@@ -31,11 +33,14 @@ struct Types<bf16> {
     using Sum = float;
     using Frag = bf16x8;   // 16 bytes of a row
     using Acc = f32x4;     // a lane's part of a 16 x 16 tile
-    template <int N>
-    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N])
+    template <int N, class F>
+    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N], F&& between)
     {
 #pragma unroll
-        for (int j = 0; j < N; ++j) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a), "v"(b[j]));
+        for (int j = 0; j < N; ++j) {
+            asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a), "v"(b[j]));
+            between(j);
+        }
     }
 };
 template <>
@@ -43,11 +48,14 @@ struct Types<f16> {
     using Sum = float;
     using Frag = f16x8;
     using Acc = f32x4;
-    template <int N>
-    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N])
+    template <int N, class F>
+    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N], F&& between)
     {
 #pragma unroll
-        for (int j = 0; j < N; ++j) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a), "v"(b[j]));
+        for (int j = 0; j < N; ++j) {
+            asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a), "v"(b[j]));
+            between(j);
+        }
     }
 };
 template <>
@@ -55,13 +63,16 @@ struct Types<float> {
     using Sum = float;
     using Frag = f32x4;
     using Acc = f32x4;
-    template <int N>
-    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N])
+    template <int N, class F>
+    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N], F&& between)
     {
 #pragma unroll
         for (int k = 0; k < 4; ++k)   // (instructions on one sum lie apart)
 #pragma unroll
-            for (int j = 0; j < N; ++j) asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a[k]), "v"(b[j][k]));
+            for (int j = 0; j < N; ++j) {
+                asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a[k]), "v"(b[j][k]));
+                if (k == 0) between(j);
+            }
     }
 };
 template <>
@@ -69,13 +80,16 @@ struct Types<double> {
     using Sum = double;
     using Frag = __attribute__((ext_vector_type(2))) double;
     using Acc = f64x4;
-    template <int N>
-    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N])
+    template <int N, class F>
+    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N], F&& between)
     {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int j = 0; j < N; ++j) c[j] = __builtin_amdgcn_mfma_f64_16x16x4f64(a[k], b[j][k], c[j], 0, 0, 0);
+            for (int j = 0; j < N; ++j) {
+                c[j] = __builtin_amdgcn_mfma_f64_16x16x4f64(a[k], b[j][k], c[j], 0, 0, 0);
+                if (k == 0) between(j);
+            }
     }
 };
 // Between instructions that write sums and instructions of other kinds that read or wrote them: more than the 19 cycles the longest of these
@@ -124,6 +138,25 @@ __device__ __forceinline__ S exp_below(S x, S m)
 // ------------------------------------------------------------------------------------------------ the products
 constexpr int kThreads = 256;   // four waves, two by two
 
+// f(std::integral_constant 0), ... f(N - 1)
+template <class F, int... I>
+__device__ __forceinline__ void unroll_(F& f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void unroll(F&& f)
+{
+    unroll_(f, std::make_integer_sequence<int, N>{});
+}
+// what is the same in all lanes, in scalar registers
+__device__ __forceinline__ const char* uniform(const char* p)
+{
+    const uint64_t v = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (const char*)(uintptr_t)((uint64_t)hi << 32 | lo);
+}
+
 struct Operands {
     const char *a, *b;
     int64_t a_pitch, b_pitch;   // bytes between rows
@@ -146,15 +179,15 @@ struct Product {
     Acc acc[SUB][SUB];
     int lane, wm, wn;
 
-    // 64 lanes' 16 bytes to LDS address `to` and behind it, past the registers.  Not counted by the compiler, which would wait for all of
-    // them before any read of LDS: the waits below are the kernel's own.  (m0 is left as it was.)
-    static __device__ __forceinline__ void load(const char* from, uint32_t to)
+    // 64 lanes' 16 bytes (at base + offset) to LDS address to + PAST and behind it, past the registers.  Not counted by the compiler, which would
+    // wait for all of them before any read of LDS: the waits below are the kernel's own.
+    template <int PAST>
+    static __device__ __forceinline__ void load(const char* base, uint32_t offset, uint32_t to)
     {
-        uint32_t kept;
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
-                     : "=&s"(kept)
-                     : "s"(to), "v"(from)
-                     : "memory");
+        asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3"
+                     :
+                     : "s"(to), "n"(PAST), "v"(offset), "s"(base)
+                     : "memory", "scc", "m0");
     }
 
     // The tile with rows m0.. of A and n0.. of B.  A step's operands lie in LDS as rows of 128 bytes, the 16-byte chunks of a row exchanged by
@@ -171,77 +204,81 @@ struct Product {
         for (int i = 0; i < SUB; ++i)
 #pragma unroll
             for (int j = 0; j < SUB; ++j) acc[i][j] = {0, 0, 0, 0};
-        const char *pa[kLoads], *pb[kLoads];
+        // (32 bits: rows of at most 4 000 000 entries, 256 or, of double, 128 of them)
+        uint32_t from_a[kLoads], from_b[kLoads];
+        const char *pa = uniform(o.a + m0 * o.a_pitch), *pb = uniform(o.b + n0 * o.b_pitch);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             // (rows behind the last are read from the last: their results are dropped)
             const int row = (i * 4 + w) * 8 + (lane >> 3), c = ((lane & 7) ^ (row & 7)) * 16;
-            pa[i] = o.a + (m0 + row < o.m ? m0 + row : o.m - 1) * o.a_pitch + c;
-            pb[i] = o.b + (n0 + row < o.n ? n0 + row : o.n - 1) * o.b_pitch + c;
+            from_a[i] = (uint32_t)((m0 + row < o.m ? row : o.m - 1 - m0) * o.a_pitch) + c;
+            from_b[i] = (uint32_t)((n0 + row < o.n ? row : o.n - 1 - n0) * o.b_pitch) + c;
         }
-        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-        auto send_one = [&](int half, int i) {
-            load(pa[i], base + half * 2 * kSide + (i * 4 + w) * 1024);
-            load(pb[i], base + half * 2 * kSide + kSide + (i * 4 + w) * 1024);
-            pa[i] += kStepBytes;
-            pb[i] += kStepBytes;
+        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + w * 1024;
+        // the i-th of a step's loads, A's and B's in turn
+        auto send = [&](int half, auto i) {
+            constexpr int k = decltype(i)::value / 2;
+            if constexpr (decltype(i)::value % 2 == 0) load<k * 4096>(pa, from_a[k], base + half * 2 * kSide);
+            else load<kSide + k * 4096>(pb, from_b[k], base + half * 2 * kSide);
         };
-        auto send = [&](int half) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) send_one(half, i);
+        auto sent = [&] {   // a whole step
+            pa += kStepBytes;
+            pb += kStepBytes;
         };
         settle(acc);
         Frag fa[2][SUB], fb[2][SUB];
         const int at = (lane & 15) * kStepBytes + (((lane >> 4) ^ (lane & 7)) << 4);
         const char *la = lds + wm * kWave * kStepBytes + at, *lb = lds + kSide + wn * kWave * kStepBytes + at;
-        // the i-th part of a half step's operands (the second half's chunks are four further on: bit 6 of the address, exchanged or not)
+        // the i-th of a half step's operands, B's and A's in turn (the second half's chunks are four further on: bit 6 of the address, exchanged
+        // or not)
         auto read = [&](int half, int kk, int i) {
-            const int to = half * 2 * kSide + i * 16 * kStepBytes;
-            fb[kk][i] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(lb - lds) ^ 64) + to : lb + to);
-            fa[kk][i] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(la - lds) ^ 64) + to : la + to);
+            const int to = half * 2 * kSide + i / 2 * 16 * kStepBytes;
+            if (i % 2 == 0) fb[kk][i / 2] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(lb - lds) ^ 64) + to : lb + to);
+            else fa[kk][i / 2] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(la - lds) ^ 64) + to : la + to);
         };
-        // step s in one half of the LDS, s + 1 in the other; more: there is a step s + 2.  What is read and sent for is strewn among the
-        // products of the row before, in the order written.
+        // Step s in one half of the LDS, s + 1 in the other; more: there is a step s + 2.  One wave per SIMD has to hide every other instruction
+        // behind its matrix instructions: one read of LDS or one load after each of them, as written.
         auto step = [&](int half, auto next, auto more) {
-#pragma unroll
-            for (int i = 0; i < SUB; ++i) {
-                if (i < SUB / 2) {
-                    read(half, 1, 2 * i);
-                    read(half, 1, 2 * i + 1);
-                }
-                Types<T>::products(fa[0][i], fb[0], acc[i]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if constexpr (decltype(next)::value) {
+            constexpr bool kNext = decltype(next)::value, kMore = decltype(more)::value;
+            constexpr int kAll = SUB * SUB;
+            unroll<SUB>([&](auto i) {
+                Types<T>::products(fa[0][i], fb[0], acc[i], [&](int j) {
+                    const int at = i * SUB + j;
+                    if (at % 2 == 0 && at / 2 < 2 * SUB) read(half, 1, at / 2);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+            if constexpr (kNext) {
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
                 __builtin_amdgcn_s_barrier();
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int i = 0; i < SUB; ++i) {
-                if constexpr (decltype(next)::value)
-                    if (i < SUB / 2) {
-                        read(half ^ 1, 0, 2 * i);
-                        read(half ^ 1, 0, 2 * i + 1);
-                    }
-                if constexpr (decltype(more)::value)
-                    if (i >= SUB / 2)
-#pragma unroll
-                        for (int l = 0; l < 2 * kLoads / SUB; ++l) send_one(half, (i - SUB / 2) * (2 * kLoads / SUB) + l);
-                Types<T>::products(fa[1][i], fb[1], acc[i]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            unroll<SUB>([&](auto i) {
+                Types<T>::products(fa[1][i], fb[1], acc[i], [&](int j) {
+                    const int at = i * SUB + j;
+                    if (kNext && at % 2 == 0 && at / 2 < 2 * SUB) read(half ^ 1, 0, at / 2);
+                    if constexpr (kMore)
+                        unroll<2 * kLoads>([&](auto l) {
+                            if (at == l * 2 + 1) send(half, l);
+                        });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+            static_assert(4 * SUB <= kAll && 4 * kLoads <= kAll);
+            if constexpr (kMore) sent();
         };
-        send(0);
+        unroll<2 * kLoads>([&](auto i) { send(0, i); });
+        sent();
         if (o.steps > 1) {
-            send(1);
+            unroll<2 * kLoads>([&](auto i) { send(1, i); });
+            sent();
             asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * kLoads) : "memory");
         } else {
             asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         }
         __builtin_amdgcn_s_barrier();
 #pragma unroll
-        for (int i = 0; i < SUB; ++i) read(0, 0, i);
+        for (int i = 0; i < 2 * SUB; ++i) read(0, 0, i);
         int half = 0;
         for (int64_t s = 2; s < o.steps; ++s) {
             step(half, std::true_type{}, std::true_type{});
@@ -259,17 +296,17 @@ struct Product {
 // Which tile a workgroup takes.  Workgroups go to the eight dies in turn, and a die's 32 compute units share a cache: a die's
 // workgroups get tiles that are neighbours, eight by four.
 struct TileOrder {
-    int64_t tiles_m, tiles_n;
+    uint32_t tiles_m, tiles_n;   // (fewer than 2^31 tiles: a grid's limit)
 };
 __device__ __forceinline__ void tile_of(const TileOrder& t, int64_t& m, int64_t& n)
 {
-    constexpr int64_t kDies = 8, kAcross = 4;
-    const int64_t all = t.tiles_m * t.tiles_n, die = blockIdx.x % kDies, each = all / kDies, more = all % kDies;
-    const int64_t at = die * each + (die < more ? die : more) + blockIdx.x / kDies;
-    const int64_t group = at / (t.tiles_m * kAcross), left = at - group * t.tiles_m * kAcross;
-    const int64_t across = t.tiles_n - group * kAcross < kAcross ? t.tiles_n - group * kAcross : kAcross;
-    m = left / across;
-    n = group * kAcross + left % across;
+    constexpr uint32_t kDies = 8, kAcross = 4;
+    const uint32_t all = t.tiles_m * t.tiles_n, die = blockIdx.x % kDies, each = all / kDies, more = all % kDies;
+    const uint32_t at = die * each + (die < more ? die : more) + blockIdx.x / kDies;
+    const uint32_t group = at / (t.tiles_m * kAcross), left = at - group * t.tiles_m * kAcross;
+    const uint32_t across = t.tiles_n - group * kAcross < kAcross ? t.tiles_n - group * kAcross : kAcross;
+    m = __builtin_amdgcn_readfirstlane(left / across);
+    n = __builtin_amdgcn_readfirstlane(group * kAcross + left % across);
 }
 
 // Forward: every row's maximum and sum of exponentials over the tile's classes (A: classes of w, B: rows of h).
@@ -651,7 +688,7 @@ TileOrder tiles_of(int64_t m, int64_t n)
 {
     constexpr int kTile = Product<T, kSub<T>>::kTile;
     static_assert(kTile >= kTileLeast && kTileRows % kTile == 0);
-    return {(m + kTile - 1) / kTile, (n + kTile - 1) / kTile};
+    return {(uint32_t)((m + kTile - 1) / kTile), (uint32_t)((n + kTile - 1) / kTile)};
 }
 // (more than 64 KiB of LDS have to be asked for, once per device)
 template <typename T, typename K, typename... Args>
@@ -660,7 +697,7 @@ hipError_t launch_product(K kernel, const TileOrder& t, hipStream_t st, const Ar
     constexpr size_t lds = Product<T, kSub<T>>::kLds;
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    kernel<<<(unsigned)(t.tiles_m * t.tiles_n), kThreads, lds, st>>>(args...);
+    kernel<<<t.tiles_m * t.tiles_n, kThreads, lds, st>>>(args...);
     return hipGetLastError();
 }
 
@@ -800,16 +837,36 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
         lay(kTileRows);
         return p;
     }
-    // Pieces as large as 512 MiB of what a class takes: the fewer there are, the less often the sums of grad_h are read and written.
+    // Pieces of at most 1 GiB of what a class takes, and of those the size for which the compute units' rounds of tiles, over all pieces and products, are
+    // fewest: 8192 rows and 4096 channels in pieces of 10240 classes have 640 tiles of grad_w, two and a half rounds that take three.
     const int64_t each = backward ? 2 * p.Tp * p.size + 2 * p.Dp * p.size : p.Dp * p.size + 2 * T * p.sum_size / kTileLeast + 1;
-    int64_t most = ((int64_t)512 << 20) / each / kTileRows * kTileRows;
-    if (most < kTileRows) most = kTileRows;
-    if (most > ((int64_t)1 << 22)) most = (int64_t)1 << 22;   // (tiles of a piece are a grid's second index)
-    for (int64_t count = (all + most - 1) / most;; ++count) {
-        const int64_t piece = ((all + count - 1) / count + kTileRows - 1) / kTileRows * kTileRows;
-        lay(piece);
-        if (ws_bytes == 0 || p.total <= ws_bytes || piece == kTileRows) return p;
+    int64_t most = ((int64_t)1 << 30) / each / kTileRows;
+    if (most < 1) most = 1;
+    if (most > (1 << 14)) most = 1 << 14;   // (tiles of a piece are a grid's second index)
+    auto fits = [&](int64_t rows) {
+        lay(rows * kTileRows);
+        return ws_bytes == 0 || p.total <= ws_bytes;
+    };
+    while (most > 1 && !fits(most)) most -= (most + 15) / 16;
+    if (most >= all / kTileRows) most = all / kTileRows;
+    int64_t best = most;
+    if (backward && most < all / kTileRows) {
+        const int64_t tile = p.size == 8 ? 128 : 256, units = 256, per_row = kTileRows / tile;
+        const int64_t tt = (T + tile - 1) / tile, td = (D + tile - 1) / tile;
+        auto rounds = [&](int64_t tiles) { return (double)((tiles + units - 1) / units); };
+        double least_cost = 1e300;
+        for (int64_t rows = most; rows > most / 2 && rows > most - 64; --rows) {
+            // a round of logits takes D steps, of grad_w T and of grad_h the piece's classes
+            const double one = rounds(rows * per_row * tt) * (double)D + rounds(rows * per_row * td) * (double)T + rounds(tt * td) * (double)(rows * kTileRows);
+            const double cost = one * (double)((all / kTileRows + rows - 1) / rows);
+            if (cost < least_cost * 0.999) {
+                least_cost = cost;
+                best = rows;
+            }
+        }
     }
+    lay(best * kTileRows);
+    return p;
 }
 
 hipError_t entropy_fwd(const EntropyPlan& p, const void* h, const void* w, const void* targets, void* loss, void* lse, double* rows,
