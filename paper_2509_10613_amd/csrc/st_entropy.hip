@@ -118,8 +118,8 @@ __device__ __forceinline__ int acc_row(int lane, int r)
 __device__ __forceinline__ double exp_of(double x, double) { return exp(x); }
 __device__ __forceinline__ float exp_of(float x, float) { return expf(x); }
 // of logits that are sums of products of 16-bit numbers: the instruction's error is far below theirs
-__device__ __forceinline__ float exp_of(float x, bf16) { return __expf(x); }
-__device__ __forceinline__ float exp_of(float x, f16) { return __expf(x); }
+__device__ __forceinline__ float exp_of(float x, bf16) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+__device__ __forceinline__ float exp_of(float x, f16) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 __device__ __forceinline__ double log_of(double x) { return log(x); }
 __device__ __forceinline__ float log_of(float x) { return logf(x); }
 
@@ -128,12 +128,19 @@ __device__ __forceinline__ S lowest()
 {
     return -(S)__builtin_inf();
 }
-// exp(x - m) where m may be the maximum of nothing
+// What is subtracted for a maximum m: exp(x - base(m)) is 0 for every x = -inf also where m is the maximum of nothing else, and NaN for NaN.
+template <typename S>
+__device__ __forceinline__ S base(S m)
+{
+    return m == lowest<S>() ? (S)0 : m;
+}
 template <typename T, typename S>
 __device__ __forceinline__ S exp_below(S x, S m)
 {
-    return m == lowest<S>() ? (S)0 : exp_of(x - m, T{});
+    return exp_of(x - base(m), T{});
 }
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }   // (not a NaN if one is a number)
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
 
 // ------------------------------------------------------------------------------------------------ the products
 constexpr int kThreads = 256;   // four waves, two by two
@@ -309,6 +316,29 @@ __device__ __forceinline__ void tile_of(const TileOrder& t, int64_t& m, int64_t&
     n = __builtin_amdgcn_readfirstlane(group * kAcross + left % across);
 }
 
+// Four lanes' four numbers turned: lane k of them gets the k-th of each, in the lanes' order.
+template <typename T>
+__device__ __forceinline__ Vec<T, 4> turn(const Vec<T, 4>& v, int lane)
+{
+    static_assert(sizeof(T) == 2);
+    uint32_t d[2];
+    __builtin_memcpy(d, &v, 8);
+    // pairs of lanes: the even one gets the lower halves (its own and the other's), the odd one the upper
+    uint32_t p[2], q[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t other = __builtin_amdgcn_mov_dpp(d[i], 0xb1, 0xf, 0xf, true);   // lane ^ 1
+        // v_perm's bytes 4 .. 7 are its first operand's
+        p[i] = lane & 1 ? __builtin_amdgcn_perm(d[i], other, 0x07060302u) : __builtin_amdgcn_perm(other, d[i], 0x05040100u);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) q[i] = __builtin_amdgcn_mov_dpp(p[i], 0x4e, 0xf, 0xf, true);   // lane ^ 2
+    const uint32_t r[2] = {lane & 2 ? q[1] : p[0], lane & 2 ? p[1] : q[0]};
+    Vec<T, 4> t;
+    __builtin_memcpy(&t, r, 8);
+    return t;
+}
+
 // Forward: every row's maximum and sum of exponentials over the tile's classes (A: classes of w, B: rows of h).
 template <typename T, int SUB>
 __global__ __launch_bounds__(kThreads, 1) void stats_kernel(Operands o, TileOrder order, const void* targets, int it, int64_t first_class, int64_t V,
@@ -341,29 +371,29 @@ __global__ __launch_bounds__(kThreads, 1) void stats_kernel(Operands o, TileOrde
         const int64_t target = row < o.n ? load_index(targets, row, it) : -1;
         const int64_t wanted64 = target >= 0 && target < V ? target - first_class - m0 - wm * kWave : -1;
         const int wanted = wanted64 >= 0 && wanted64 < kWave ? (int)wanted64 : -1;   // of this wave's classes
-        S top = lowest<S>(), mine = 0;
-        bool found = false;
+        if (__any(wanted >= 0)) {   // (of few tiles)
+            S mine = 0;
+#pragma unroll
+            for (int i = 0; i < SUB; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mine = i * 16 + acc_row<T>(lane, r) == wanted ? acc[i][j][r] : mine;
+            // (of the four lanes that share the row, the one that holds the class)
+            if (wanted >= 0 && (sizeof(T) == 8 ? wanted & 3 : wanted >> 2 & 3) == lane >> 4) hit[row] = mine;
+        }
+        // NaN passes by the maximum, and through the sum
+        S top = lowest<S>();
 #pragma unroll
         for (int i = 0; i < SUB; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const S z = acc[i][j][r];
-                const bool here = i * 16 + acc_row<T>(lane, r) == wanted;
-                mine = here ? z : mine;
-                found |= here;
-                top = z > top || z != z ? z : top;   // (a maximum that a NaN passes through)
-            }
-        if (found) hit[row] = mine;
-#pragma unroll
-        for (int x = 16; x < 64; x *= 2) {
-            const S other = __shfl_xor(top, x);
-            top = other > top || other != other ? other : top;
-        }
+            for (int r = 0; r < 4; ++r) top = larger(acc[i][j][r], top);
+        top = larger(top, __shfl_xor(top, 16));
+        top = larger(top, __shfl_xor(top, 32));
+        const S from = base(top);
         S sum = 0;
 #pragma unroll
         for (int i = 0; i < SUB; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += exp_below<T>(acc[i][j][r], top);
+            for (int r = 0; r < 4; ++r) sum += exp_of(acc[i][j][r] - from, T{});
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (lane < 16) {
@@ -376,7 +406,7 @@ __global__ __launch_bounds__(kThreads, 1) void stats_kernel(Operands o, TileOrde
     const int64_t row = n0 + threadIdx.x;
     if (threadIdx.x < kTile && row < o.n) {
         const S a = waves[threadIdx.x], b = waves[2 * kTile + threadIdx.x];
-        const S top = b > a || b != b ? b : a;
+        const S top = larger(a, b);
         part_max[tile_m * o.n + row] = top;
         part_sum[tile_m * o.n + row] =
             waves[kTile + threadIdx.x] * exp_below<T>(a, top) + waves[3 * kTile + threadIdx.x] * exp_below<T>(b, top);
@@ -409,29 +439,43 @@ __global__ __launch_bounds__(kThreads, 1) void grads_kernel(Operands o, TileOrde
         const int64_t wanted64 = target - first_class - m0 - wm * kWave;
         const int wanted = wanted64 >= 0 && wanted64 < kWave ? (int)wanted64 : -1;
         const S u = there ? up[row] : (S)0, l = there ? lse[row] : (S)0;
+        const bool some = u != 0, any = __any(wanted >= 0);
+        T* g_at = g + row * g_pitch + m0 + wm * kWave + acc_row<T>(lane, 0);
+        // (16-bit types: four lanes hold four classes of four rows, and each takes one class of the four rows)
+        const int64_t turned = sizeof(T) == 2 ? row - (lane & 3) : row;
+        T* gt_at = gt + (m0 + wm * kWave + acc_row<T>(lane, 0) + (sizeof(T) == 2 ? lane & 3 : 0)) * gt_pitch + turned;
 #pragma unroll
         for (int i = 0; i < SUB; ++i) {
             const int64_t cls = m0 + wm * kWave + i * 16;
+            S x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = u * exp_of(acc[i][j][r] - l, T{});
+            if (any)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = i * 16 + acc_row<T>(lane, r) == wanted ? u * (exp_of(acc[i][j][r] - l, T{}) - (S)1) : x[r];
+            if (!inside)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = cls + acc_row<T>(lane, r) < o.m ? x[r] : (S)0;
             Vec<T, 4> v;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int at = acc_row<T>(lane, r);
-                const S p = exp_of(acc[i][j][r] - l, T{}) - (i * 16 + at == wanted ? (S)1 : (S)0);
-                // rows without a target (u is 0) stay 0 whatever their logits are
-                v.v[r] = (T)(u != 0 && (inside || cls + at < o.m) ? u * p : (S)0);
-            }
+            for (int r = 0; r < 4; ++r) v.v[r] = (T)(some ? x[r] : (S)0);   // rows without a target stay 0 whatever their logits are
             if constexpr (sizeof(T) == 8) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (there && cls + acc_row<T>(lane, r) < g_pitch) g[row * g_pitch + cls + acc_row<T>(lane, r)] = v.v[r];
+                    if (there && cls + acc_row<T>(lane, r) < g_pitch) g_at[i * 16 + 4 * r] = v.v[r];
             } else {
                 // (g_pitch is a multiple of 16: the tile is in or out)
-                if (there && cls < g_pitch) store_vec(g + row * g_pitch + cls + acc_row<T>(lane, 0), v);
+                if (there && cls < g_pitch) store_vec(g_at + i * 16, v);
             }
-            if (row < gt_pitch)
+            if constexpr (sizeof(T) == 2) {
+                // (gt_pitch is a multiple of 64)
+                const Vec<T, 4> t = turn(v, lane);
+                if (turned < gt_pitch && (inside || cls + acc_row<T>(lane, 0) + (lane & 3) < o.m)) store_vec(gt_at + i * 16 * gt_pitch, t);
+            } else if (row < gt_pitch) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (inside || cls + acc_row<T>(lane, r) < o.m) gt[(cls + acc_row<T>(lane, r)) * gt_pitch + row] = v.v[r];
+                    if (inside || cls + acc_row<T>(lane, r) < o.m) gt_at[(i * 16 + acc_row<T>(0, r)) * gt_pitch] = v.v[r];
+            }
         }
     }
 }
@@ -519,26 +563,40 @@ __global__ __launch_bounds__(256) void zero_kernel(T* p, int64_t n)
 }
 
 // dst[cols][pitch] = src[rows][cols] transposed, zeros behind the rows.  targets not null: rows without one are zeros, whatever they hold.
+// A workgroup turns 64 x 64 entries (32 x 64 of double), moved as 16 bytes either way.
+template <typename T>
+constexpr int kTurnCols = sizeof(T) == 8 ? 32 : 64;
 template <typename T>
 __global__ __launch_bounds__(256) void transpose_kernel(const T* src, T* dst, int64_t rows, int64_t cols, int64_t pitch, const void* targets,
                                                         int it, int64_t V)
 {
-    constexpr int N = 64;
-    __shared__ T tile[N][N + 16 / sizeof(T) / 2];
-    const int64_t r0 = (int64_t)blockIdx.x * N, c0 = (int64_t)blockIdx.y * N;
-    for (int i = threadIdx.x; i < N * N; i += 256) {
-        const int64_t r = r0 + i / N, c = c0 + i % N;
-        bool there = r < rows && c < cols;
+    constexpr int R = 64, C = kTurnCols<T>, E = kPer16<T>, kPad = 4 / sizeof(T) ? 4 / sizeof(T) : 1;
+    __shared__ T tile[C][R + kPad];   // (an odd number of words from column to column, or of double words)
+    const int64_t r0 = (int64_t)blockIdx.x * R, c0 = (int64_t)blockIdx.y * C;
+    for (int i = threadIdx.x; i < R * C / E; i += 256) {
+        const int row = i / (C / E), col = i % (C / E) * E;
+        const int64_t r = r0 + row, left = cols - c0 - col;
+        bool there = r < rows && left > 0;
         if (there && targets) {
             const int64_t t = load_index(targets, r, it);
             there = t >= 0 && t < V;
         }
-        tile[i / N][i % N] = there ? src[r * cols + c] : T(0);
+        Vec<T, E> v;
+        const T* from = src + r * cols + c0 + col;
+        if (there && left >= E) v = load_vec<T, E>(from);
+        else v = load_some<T, E>(from, there ? (int)left : 0);
+#pragma unroll
+        for (int e = 0; e < E; ++e) tile[col + e][row] = v.v[e];
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < N * N; i += 256) {
-        const int64_t r = r0 + i % N, c = c0 + i / N;
-        if (c < cols && r < pitch) dst[c * pitch + r] = tile[i % N][i / N];
+    for (int i = threadIdx.x; i < R * C / E; i += 256) {
+        const int col = i / (R / E), row = i % (R / E) * E;
+        // (the pitch is a multiple of 16 bytes)
+        if (c0 + col >= cols || r0 + row >= pitch) continue;
+        Vec<T, E> v;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v.v[e] = tile[col][row + e];
+        store_vec(dst + (c0 + col) * pitch + r0 + row, v);
     }
 }
 
@@ -557,7 +615,7 @@ __global__ __launch_bounds__(1024) void join_kernel(const typename Types<T>::Sum
     const int64_t row = (int64_t)blockIdx.x * 64 + lane;
     S top = lowest<S>(), sum = 0;
     auto add = [&](S t, S s) {
-        const S m = t > top || t != t ? t : top;
+        const S m = larger(t, top);
         sum = sum * exp_below<T>(top, m) + s * exp_below<T>(t, m);
         top = m;
     };
@@ -749,7 +807,7 @@ hipError_t run_bwd(const EntropyPlan& p, const T* h, const T* w, const void* tar
     hipError_t e = in_steps(h, p.T, p.D, p.Dp, ws + p.off_h, &hs, st);
     if (e != hipSuccess) return e;
     auto turn = [&](const T* src, T* dst, int64_t r, int64_t pitch, const void* only) -> hipError_t {
-        ST_TRY((transpose_kernel<T><<<dim3((unsigned)((pitch + 63) / 64), (unsigned)((p.D + 63) / 64)), 256, 0, st>>>(src, dst, r, p.D, pitch, only, it,
+        ST_TRY((transpose_kernel<T><<<dim3((unsigned)((pitch + 63) / 64), (unsigned)((p.D + kTurnCols<T> - 1) / kTurnCols<T>)), 256, 0, st>>>(src, dst, r, p.D, pitch, only, it,
                                                                                                                   p.V)));
         return hipSuccess;
     };
@@ -864,6 +922,10 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
                 best = rows;
             }
         }
+    }
+    if (!backward) {   // of about the same size
+        const int64_t count = (all / kTileRows + most - 1) / most;
+        best = (all / kTileRows + count - 1) / count;
     }
     lay(best * kTileRows);
     return p;
