@@ -42,13 +42,15 @@ struct EntropyPlan {
     int size, sum_size;        // bytes of an element and of a sum
     int64_t Dp, Tp;            // D and T in whole steps
     int64_t piece, pieces;     // classes per piece (a multiple of kTileRows)
+    int64_t parts;             // backward: workgroups per tile of grad_h, which divide a piece's classes
+    bool sums;                 // ... and whether grad_h is summed over pieces or parts
     size_t off_h, off_w;       // copies of h and of a piece of w with rows of Dp (used where the caller's do not fit)
     size_t off_max, off_sum, off_hit;   // forward: running maximum and sum, and the target's logit, of every row
     size_t off_part;           // ... and those of the piece's tiles
     size_t off_up;             // backward: every row's upstream gradient (and behind them the scaling, two numbers)
     size_t off_ht, off_wt;     // ... h and a piece of w transposed
     size_t off_g, off_gt;      // ... the piece's gradients of the logits, as they are and transposed
-    size_t off_dh;             // ... the sum of grad_h over the pieces
+    size_t off_dh;             // ... the sums of grad_h, one per part
     size_t total;
 };
 // ws_bytes 0: as fast as it gets; otherwise pieces that fit it.  least: the smallest pieces.
