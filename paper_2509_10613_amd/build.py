@@ -15,16 +15,18 @@ SOURCES = ["sk_api.hip", "sk_kernels.hip", "sk_lockstep.hip", "sk_solo.hip", "sk
 HEADERS = ["sk_plan.h", "sk_band.h", "sk_kernels.h", "sk_dev.h", "sk_lane.h", "sk_solo_impl.h", "sk_tile.h", "sk_quad.h", "sg_plan.h", "sg_kernels.h", "sg_dev.h"]
 PUBLIC = ["sigkernel.h", "signature.h"]
 # The operators of sigtrain.h: sources and headers of their own, so that a change to either half leaves the other's objects alone.
-TRAIN_SOURCES = ["st_api.hip", "st_embed.hip", "st_entropy.hip", "st_clip.hip"]
-TRAIN_HEADERS = ["st_kernels.h", "st_dev.h", "sk_error.h"]
+TRAIN_SOURCES = ["st_api.hip", "st_embed.hip", "st_entropy.hip", "st_entropy_bf16.hip", "st_entropy_f16.hip", "st_entropy_f32.hip", "st_entropy_f64.hip",
+                 "st_clip.hip"]
+TRAIN_HEADERS = ["st_kernels.h", "st_dev.h", "st_entropy_impl.h", "sk_error.h"]
 TRAIN_PUBLIC = ["sigkernel.h", "sigtrain.h"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 # Per source file.  The tile backward kernel moves every MFMA result on (to LDS, to atomics): with the results in
 # vector registers instead of accumulation registers the copies between the two fall away (c5 backward: -1 %).
-# st_entropy.hip says that its loads to LDS change m0, which the compiler keeps nothing in and warns of.
-FILE_FLAGS = {"sk_tile_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "st_entropy.hip": ["-Wno-inline-asm"]}
+# The products of st_entropy_impl.h say that their loads to LDS change m0, which the compiler keeps nothing in and warns of.
+FILE_FLAGS = {"sk_tile_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+              **{"st_entropy_%s.hip" % t: ["-Wno-inline-asm"] for t in ("bf16", "f16", "f32", "f64")}}
 
 
 def _stale(target, deps):

@@ -1,932 +1,44 @@
-// Softmax cross entropy of a linear read-out, and its gradients, in pieces of the classes.
-//
-// Forward: the logits z = h w^T are formed tile by tile on the matrix cores and reduced in registers to every row's maximum and sum
-// of exponentials over the tile (and the target's logit); no logit is written.  Backward: the logits of a piece of the classes are formed
-// again, their gradients G = u (exp(z - lse) - [class = target]) written as they are and transposed, and multiplied: grad_h += G w and
-// grad_w = G^T h.
-//
-// All products are of one form, C[m, n] = sum_k A[m, k] B[n, k] with rows of A and B in whole steps of 128 bytes, so one main loop serves
-// every type: a lane holds 16 consecutive bytes of a row, which are one matrix instruction's operand for 16-bit types and four or two
-// instructions' for float and double (the order of k does not matter as long as both sides have the same).  The side whose index the
-// result's rows run along is B: a lane then holds results that lie side by side in a row.
+// Cross entropy of a linear read-out: the pieces, tiles and scratch of a call (the kernels: st_entropy_impl.h, compiled for each type).
 #include <algorithm>
-#include <utility>
 
 #include "st_dev.h"
 #include "st_kernels.h"
 
 namespace st {
+
+template <typename T>
+hipError_t entropy_run_fwd(const EntropyPlan& p, const T* h, const T* w, const void* targets, void* loss, void* lse, double* rows, int reduction, int it,
+                           unsigned char* ws, hipStream_t st);
+template <typename T>
+hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const void* targets, const void* lse, const double* rows, const void* grad,
+                           T* grad_h, T* grad_w, int reduction, int it, unsigned char* ws, hipStream_t st);
+
 namespace {
 
-using f32x4 = __attribute__((ext_vector_type(4))) float;
-using f64x4 = __attribute__((ext_vector_type(4))) double;
-using bf16x8 = __attribute__((ext_vector_type(8))) bf16;
-using f16x8 = __attribute__((ext_vector_type(8))) f16;
-
-// c[j] += a b[j]^T; between(j) after the j-th: the other instructions that hide behind the matrix instructions.  Sums of float stay in the accumulation registers for as long as the products last: the instructions are written out, since the
-// compiler, left to place 256 sums and the operands of two steps, moves hundreds of registers between the two files in every step (128 x 128
-// classes and rows per wave: 960 against 1290 TFLOP/s).  What the compiler would wait for, `settle` does; operands come from
-// LDS, whose loads it waits for as for any instruction's.
-template <typename T>
-struct Types;
-template <>
-struct Types<bf16> {
-    using Sum = float;
-    using Frag = bf16x8;   // 16 bytes of a row
-    using Acc = f32x4;     // a lane's part of a 16 x 16 tile
-    template <int N, class F>
-    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N], F&& between)
-    {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a), "v"(b[j]));
-            between(j);
-        }
-    }
-};
-template <>
-struct Types<f16> {
-    using Sum = float;
-    using Frag = f16x8;
-    using Acc = f32x4;
-    template <int N, class F>
-    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N], F&& between)
-    {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a), "v"(b[j]));
-            between(j);
-        }
-    }
-};
-template <>
-struct Types<float> {
-    using Sum = float;
-    using Frag = f32x4;
-    using Acc = f32x4;
-    template <int N, class F>
-    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N], F&& between)
-    {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)   // (instructions on one sum lie apart)
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a[k]), "v"(b[j][k]));
-                if (k == 0) between(j);
-            }
-    }
-};
-template <>
-struct Types<double> {
-    using Sum = double;
-    using Frag = __attribute__((ext_vector_type(2))) double;
-    using Acc = f64x4;
-    template <int N, class F>
-    static __device__ __forceinline__ void products(Frag a, const Frag (&b)[N], Acc (&c)[N], F&& between)
-    {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                c[j] = __builtin_amdgcn_mfma_f64_16x16x4f64(a[k], b[j][k], c[j], 0, 0, 0);
-                if (k == 0) between(j);
-            }
-    }
-};
-// Between instructions that write sums and instructions of other kinds that read or wrote them: more than the 19 cycles the longest of these
-// matrix instructions' results take.
-template <int M, int N>
-__device__ __forceinline__ void settle(f32x4 (&acc)[M][N])
+// The tiles of a product of m by n results over `steps`, on 256 compute units: of the sizes there are, divided among up to most_parts workgroups
+// each (which leave sums, to be added by another launch), those that take the fewest cycles by this estimate.
+// A step of a tile of 32 sub by 32 sub takes 32 sub^2 cycles of matrix instructions (16-bit types; 1.35 times that as measured; float and double
+// eight times as many), or what arrives at 40 bytes a cycle, and with one workgroup on a compute unit no less than the way to memory and back.
+Tiling choose_tiling(int size, int64_t m, int64_t n, int64_t steps, int64_t most_parts, int sum_size)
 {
-#pragma unroll
-    for (int i = 0; i < M; ++i)
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (i + j == 0) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[i][j]));
-            else asm volatile("" : "+a"(acc[i][j]));
-}
-template <int M, int N>
-__device__ __forceinline__ void settle(f64x4 (&)[M][N])
-{
-}
-// The row of a 16 x 16 result tile that a lane's r-th number belongs to (its column is lane % 16).
-template <typename T>
-__device__ __forceinline__ int acc_row(int lane, int r)
-{
-    return sizeof(T) == 8 ? (lane >> 4) + 4 * r : (lane >> 4) * 4 + r;
-}
-
-__device__ __forceinline__ double exp_of(double x, double) { return exp(x); }
-__device__ __forceinline__ float exp_of(float x, float) { return expf(x); }
-// of logits that are sums of products of 16-bit numbers: the instruction's error is far below theirs
-__device__ __forceinline__ float exp_of(float x, bf16) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
-__device__ __forceinline__ float exp_of(float x, f16) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
-__device__ __forceinline__ double log_of(double x) { return log(x); }
-__device__ __forceinline__ float log_of(float x) { return logf(x); }
-
-template <typename S>
-__device__ __forceinline__ S lowest()
-{
-    return -(S)__builtin_inf();
-}
-// What is subtracted for a maximum m: exp(x - base(m)) is 0 for every x = -inf also where m is the maximum of nothing else, and NaN for NaN.
-template <typename S>
-__device__ __forceinline__ S base(S m)
-{
-    return m == lowest<S>() ? (S)0 : m;
-}
-template <typename T, typename S>
-__device__ __forceinline__ S exp_below(S x, S m)
-{
-    return exp_of(x - base(m), T{});
-}
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }   // (not a NaN if one is a number)
-__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
-
-// ------------------------------------------------------------------------------------------------ the products
-constexpr int kThreads = 256;   // four waves, two by two
-
-// f(std::integral_constant 0), ... f(N - 1)
-template <class F, int... I>
-__device__ __forceinline__ void unroll_(F& f, std::integer_sequence<int, I...>)
-{
-    (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, class F>
-__device__ __forceinline__ void unroll(F&& f)
-{
-    unroll_(f, std::make_integer_sequence<int, N>{});
-}
-// what is the same in all lanes, in scalar registers
-__device__ __forceinline__ const char* uniform(const char* p)
-{
-    const uint64_t v = (uint64_t)(uintptr_t)p;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-    return (const char*)(uintptr_t)((uint64_t)hi << 32 | lo);
-}
-
-struct Operands {
-    const char *a, *b;
-    int64_t a_pitch, b_pitch;   // bytes between rows
-    int64_t m, n;               // rows
-    int64_t steps;              // of kStepBytes along k
-};
-
-// A wave's tile is SUB x SUB tiles of 16 x 16, a workgroup's twice that on either side.  Large tiles read least from LDS per product: 128 x 128
-// per wave (256 x 256 per workgroup) take 1024 of the 2048 cycles a step's matrix instructions last, and 512 for the loads that arrive.  That is
-// 256 registers of sums (float; double sums take twice as many, so half the tile on either side).
-template <typename T, int SUB>
-struct Product {
-    using Frag = typename Types<T>::Frag;
-    using Acc = typename Types<T>::Acc;
-    static constexpr int kWave = SUB * 16, kTile = 2 * kWave;
-    static constexpr int kSide = kTile * kStepBytes;           // bytes of one operand's step in LDS
-    static constexpr size_t kLds = 4 * kSide;                  // two steps of two operands
-    static constexpr int kLoads = kSide / (16 * kThreads);     // 16-byte loads per thread, side and step
-
-    Acc acc[SUB][SUB];
-    int lane, wm, wn;
-
-    // 64 lanes' 16 bytes (at base + offset) to LDS address to + PAST and behind it, past the registers.  Not counted by the compiler, which would
-    // wait for all of them before any read of LDS: the waits below are the kernel's own.
-    template <int PAST>
-    static __device__ __forceinline__ void load(const char* base, uint32_t offset, uint32_t to)
-    {
-        asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3"
-                     :
-                     : "s"(to), "n"(PAST), "v"(offset), "s"(base)
-                     : "memory", "scc", "m0");
-    }
-
-    // The tile with rows m0.. of A and n0.. of B.  A step's operands lie in LDS as rows of 128 bytes, the 16-byte chunks of a row exchanged by
-    // its number modulo 8, so that eight rows' chunks of one column lie in different banks.  Two steps are under way: a wave reads the second half
-    // of step s, multiplies the first half, and after the one barrier of a step (everybody has read step s, step s + 1 has arrived) sends for
-    // step s + 2, reads the first half of step s + 1 and multiplies the second half of step s.
-    __device__ __forceinline__ void run(const Operands& o, int64_t m0, int64_t n0, char* lds)
-    {
-        lane = threadIdx.x & 63;
-        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        wm = w >> 1;
-        wn = w & 1;
-#pragma unroll
-        for (int i = 0; i < SUB; ++i)
-#pragma unroll
-            for (int j = 0; j < SUB; ++j) acc[i][j] = {0, 0, 0, 0};
-        // (32 bits: rows of at most 4 000 000 entries, 256 or, of double, 128 of them)
-        uint32_t from_a[kLoads], from_b[kLoads];
-        const char *pa = uniform(o.a + m0 * o.a_pitch), *pb = uniform(o.b + n0 * o.b_pitch);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            // (rows behind the last are read from the last: their results are dropped)
-            const int row = (i * 4 + w) * 8 + (lane >> 3), c = ((lane & 7) ^ (row & 7)) * 16;
-            from_a[i] = (uint32_t)((m0 + row < o.m ? row : o.m - 1 - m0) * o.a_pitch) + c;
-            from_b[i] = (uint32_t)((n0 + row < o.n ? row : o.n - 1 - n0) * o.b_pitch) + c;
-        }
-        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + w * 1024;
-        // the i-th of a step's loads, A's and B's in turn
-        auto send = [&](int half, auto i) {
-            constexpr int k = decltype(i)::value / 2;
-            if constexpr (decltype(i)::value % 2 == 0) load<k * 4096>(pa, from_a[k], base + half * 2 * kSide);
-            else load<kSide + k * 4096>(pb, from_b[k], base + half * 2 * kSide);
-        };
-        auto sent = [&] {   // a whole step
-            pa += kStepBytes;
-            pb += kStepBytes;
-        };
-        settle(acc);
-        Frag fa[2][SUB], fb[2][SUB];
-        const int at = (lane & 15) * kStepBytes + (((lane >> 4) ^ (lane & 7)) << 4);
-        const char *la = lds + wm * kWave * kStepBytes + at, *lb = lds + kSide + wn * kWave * kStepBytes + at;
-        // the i-th of a half step's operands, B's and A's in turn (the second half's chunks are four further on: bit 6 of the address, exchanged
-        // or not)
-        auto read = [&](int half, int kk, int i) {
-            const int to = half * 2 * kSide + i / 2 * 16 * kStepBytes;
-            if (i % 2 == 0) fb[kk][i / 2] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(lb - lds) ^ 64) + to : lb + to);
-            else fa[kk][i / 2] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(la - lds) ^ 64) + to : la + to);
-        };
-        // Step s in one half of the LDS, s + 1 in the other; more: there is a step s + 2.  One wave per SIMD has to hide every other instruction
-        // behind its matrix instructions: one read of LDS or one load after each of them, as written.
-        auto step = [&](int half, auto next, auto more) {
-            constexpr bool kNext = decltype(next)::value, kMore = decltype(more)::value;
-            constexpr int kAll = SUB * SUB;
-            unroll<SUB>([&](auto i) {
-                Types<T>::products(fa[0][i], fb[0], acc[i], [&](int j) {
-                    const int at = i * SUB + j;
-                    if (at % 2 == 0 && at / 2 < 2 * SUB) read(half, 1, at / 2);
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-            });
-            if constexpr (kNext) {
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
-                __builtin_amdgcn_s_barrier();
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            unroll<SUB>([&](auto i) {
-                Types<T>::products(fa[1][i], fb[1], acc[i], [&](int j) {
-                    const int at = i * SUB + j;
-                    if (kNext && at % 2 == 0 && at / 2 < 2 * SUB) read(half ^ 1, 0, at / 2);
-                    if constexpr (kMore)
-                        unroll<2 * kLoads>([&](auto l) {
-                            if (at == l * 2 + 1) send(half, l);
-                        });
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-            });
-            static_assert(4 * SUB <= kAll && 4 * kLoads <= kAll);
-            if constexpr (kMore) sent();
-        };
-        unroll<2 * kLoads>([&](auto i) { send(0, i); });
-        sent();
-        if (o.steps > 1) {
-            unroll<2 * kLoads>([&](auto i) { send(1, i); });
-            sent();
-            asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * kLoads) : "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        }
-        __builtin_amdgcn_s_barrier();
-#pragma unroll
-        for (int i = 0; i < 2 * SUB; ++i) read(0, 0, i);
-        int half = 0;
-        for (int64_t s = 2; s < o.steps; ++s) {
-            step(half, std::true_type{}, std::true_type{});
-            half ^= 1;
-        }
-        if (o.steps > 1) {
-            step(half, std::true_type{}, std::false_type{});
-            half ^= 1;
-        }
-        step(half, std::false_type{}, std::false_type{});
-        settle(acc);
-        __syncthreads();   // (what follows may use the LDS)
-    }
-};
-// Which tile a workgroup takes.  Workgroups go to the eight dies in turn, and a die's 32 compute units share a cache: a die's
-// workgroups get tiles that are neighbours, eight by four.
-struct TileOrder {
-    uint32_t tiles_m, tiles_n;   // (fewer than 2^31 workgroups: a grid's limit)
-    uint32_t parts = 1;          // workgroups per tile, which lie one behind the other
-};
-__device__ __forceinline__ int tile_of(const TileOrder& t, int64_t& m, int64_t& n)
-{
-    constexpr uint32_t kDies = 8, kAcross = 4;
-    const uint32_t all = t.tiles_m * t.tiles_n * t.parts, die = blockIdx.x % kDies, each = all / kDies, more = all % kDies;
-    const uint32_t place = die * each + (die < more ? die : more) + blockIdx.x / kDies, at = place / t.parts;
-    const uint32_t group = at / (t.tiles_m * kAcross), left = at - group * t.tiles_m * kAcross;
-    const uint32_t across = t.tiles_n - group * kAcross < kAcross ? t.tiles_n - group * kAcross : kAcross;
-    m = __builtin_amdgcn_readfirstlane(left / across);
-    n = __builtin_amdgcn_readfirstlane(group * kAcross + left % across);
-    return __builtin_amdgcn_readfirstlane(place - at * t.parts);
-}
-
-// Four lanes' four numbers turned: lane k of them gets the k-th of each, in the lanes' order.
-template <typename T>
-__device__ __forceinline__ Vec<T, 4> turn(const Vec<T, 4>& v, int lane)
-{
-    static_assert(sizeof(T) == 2);
-    uint32_t d[2];
-    __builtin_memcpy(d, &v, 8);
-    // pairs of lanes: the even one gets the lower halves (its own and the other's), the odd one the upper
-    uint32_t p[2], q[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t other = __builtin_amdgcn_mov_dpp(d[i], 0xb1, 0xf, 0xf, true);   // lane ^ 1
-        // v_perm's bytes 4 .. 7 are its first operand's
-        p[i] = lane & 1 ? __builtin_amdgcn_perm(d[i], other, 0x07060302u) : __builtin_amdgcn_perm(other, d[i], 0x05040100u);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) q[i] = __builtin_amdgcn_mov_dpp(p[i], 0x4e, 0xf, 0xf, true);   // lane ^ 2
-    const uint32_t r[2] = {lane & 2 ? q[1] : p[0], lane & 2 ? p[1] : q[0]};
-    Vec<T, 4> t;
-    __builtin_memcpy(&t, r, 8);
-    return t;
-}
-
-// Results of 16 bits leave through LDS, as whole rows of the tile: straight from the registers a store takes 32 bytes each of 16 rows, and the
-// logits' gradients cost 1.04 ms instead of @@ for 8192 rows and 16384 classes.  The tile's rows lie in LDS one behind the other, their 16-byte chunks
-// exchanged by the row's number, so that neither direction meets one bank twice.
-template <typename T, int TILE>
-struct Outbox {
-    static_assert(sizeof(T) == 2);
-    static constexpr int kChunks = TILE / 8;
-    char* lds;
-    // four entries from column `col` (a multiple of four) on
-    __device__ __forceinline__ void put(int row, int col, const Vec<T, 4>& v) const
-    {
-        __builtin_memcpy(__builtin_assume_aligned(lds + row * (TILE * 2) + (((col >> 3) ^ (row & (kChunks - 1))) << 4) + (col & 4) * 2, 8), &v, 8);
-    }
-    // the whole tile, between two barriers; `cols` columns are left in the rows of `out`
-    __device__ __forceinline__ void send(T* out, int64_t pitch, int64_t rows, int64_t cols) const
-    {
-        __syncthreads();
-        const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-        constexpr int kRows = 64 / kChunks;   // per wave and store
-#pragma unroll 4
-        for (int i = 0; i < TILE / (4 * kRows); ++i) {
-            const int row = (i * 4 + w) * kRows + lane / kChunks, chunk = lane % kChunks;
-            Vec<T, 8> v;
-            __builtin_memcpy(&v, __builtin_assume_aligned(lds + row * (TILE * 2) + ((chunk ^ (row & (kChunks - 1))) << 4), 16), 16);
-            if (row >= rows) continue;
-            T* to = out + row * pitch + chunk * 8;
-            const int64_t left = cols - chunk * 8;
-            if (left >= 8) store_vec(to, v);
-            else if (left > 0) store_some(to, v, (int)left);
-        }
-        __syncthreads();
-    }
-};
-
-// A result in the arrays' type; a 0 stays one whatever is upstream (rows without a target).
-template <typename T, typename S>
-__device__ __forceinline__ T scaled(S x, S f)
-{
-    return (T)(x == 0 ? x : x * f);
-}
-struct NoOutbox {
-    char* lds;
-};
-template <typename T, int TILE>
-using OutboxOf = typename std::conditional_t<sizeof(T) == 2, std::enable_if<true, Outbox<std::conditional_t<sizeof(T) == 2, T, bf16>, TILE>>,
-                                             std::enable_if<true, NoOutbox>>::type;
-
-// Forward: every row's maximum and sum of exponentials over the tile's classes (A: classes of w, B: rows of h).
-template <typename T, int SUB>
-__global__ __launch_bounds__(kThreads, 1) void stats_kernel(Operands o, TileOrder order, const void* targets, int it, int64_t first_class, int64_t V,
-                                                         typename Types<T>::Sum* part_max, typename Types<T>::Sum* part_sum,
-                                                         typename Types<T>::Sum* hit)
-{
-    using S = typename Types<T>::Sum;
-    using P = Product<T, SUB>;
-    constexpr int kTile = P::kTile, kWave = P::kWave;
-    extern __shared__ __align__(16) char lds[];
-    int64_t tile_m, tile_n;
-    tile_of(order, tile_m, tile_n);
-    const int64_t m0 = tile_m * kTile, n0 = tile_n * kTile;
-    P p;
-    p.run(o, m0, n0, lds);
-    auto& acc = p.acc;
-    const int lane = p.lane, wm = p.wm, wn = p.wn;
-    S* waves = reinterpret_cast<S*>(lds);   // [2 halves of the classes][2: maximum, sum][kTile]
-    if (m0 + kTile > o.m)   // classes behind the last
-#pragma unroll
-        for (int i = 0; i < SUB; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (m0 + wm * kWave + i * 16 + acc_row<T>(lane, r) >= o.m)
-#pragma unroll
-                    for (int j = 0; j < SUB; ++j) acc[i][j][r] = lowest<S>();
-#pragma unroll
-    for (int j = 0; j < SUB; ++j) {
-        const int64_t row = n0 + wn * kWave + j * 16 + (lane & 15);
-        const int64_t target = row < o.n ? load_index(targets, row, it) : -1;
-        const int64_t wanted64 = target >= 0 && target < V ? target - first_class - m0 - wm * kWave : -1;
-        const int wanted = wanted64 >= 0 && wanted64 < kWave ? (int)wanted64 : -1;   // of this wave's classes
-        if (__any(wanted >= 0)) {   // (of few tiles)
-            S mine = 0;
-#pragma unroll
-            for (int i = 0; i < SUB; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) mine = i * 16 + acc_row<T>(lane, r) == wanted ? acc[i][j][r] : mine;
-            // (of the four lanes that share the row, the one that holds the class)
-            if (wanted >= 0 && (sizeof(T) == 8 ? wanted & 3 : wanted >> 2 & 3) == lane >> 4) hit[row] = mine;
-        }
-        // NaN passes by the maximum, and through the sum
-        S top = lowest<S>();
-#pragma unroll
-        for (int i = 0; i < SUB; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) top = larger(acc[i][j][r], top);
-        top = larger(top, __shfl_xor(top, 16));
-        top = larger(top, __shfl_xor(top, 32));
-        const S from = base(top);
-        S sum = 0;
-#pragma unroll
-        for (int i = 0; i < SUB; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) sum += exp_of(acc[i][j][r] - from, T{});
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (lane < 16) {
-            waves[(wm * 2 + 0) * kTile + wn * kWave + j * 16 + lane] = top;
-            waves[(wm * 2 + 1) * kTile + wn * kWave + j * 16 + lane] = sum;
-        }
-    }
-    __syncthreads();
-    static_assert(kTile <= kThreads);
-    const int64_t row = n0 + threadIdx.x;
-    if (threadIdx.x < kTile && row < o.n) {
-        const S a = waves[threadIdx.x], b = waves[2 * kTile + threadIdx.x];
-        const S top = larger(a, b);
-        part_max[tile_m * o.n + row] = top;
-        part_sum[tile_m * o.n + row] =
-            waves[kTile + threadIdx.x] * exp_below<T>(a, top) + waves[3 * kTile + threadIdx.x] * exp_below<T>(b, top);
-    }
-}
-
-// Backward: the gradients of the piece's logits, g[row][class] and gt[class][row], zeros up to whole steps.
-template <typename T, int SUB>
-__global__ __launch_bounds__(kThreads, 1) void grads_kernel(Operands o, TileOrder order, const void* targets, int it, int64_t first_class,
-                                                         const typename Types<T>::Sum* lse, const typename Types<T>::Sum* up, T* g,
-                                                         int64_t g_pitch, T* gt, int64_t gt_pitch)
-{
-    using S = typename Types<T>::Sum;
-    using P = Product<T, SUB>;
-    constexpr int kTile = P::kTile, kWave = P::kWave;
-    extern __shared__ __align__(16) char lds[];
-    int64_t tile_m, tile_n;
-    tile_of(order, tile_m, tile_n);
-    const int64_t m0 = tile_m * kTile, n0 = tile_n * kTile;
-    P p;
-    p.run(o, m0, n0, lds);
-    auto& acc = p.acc;
-    const int lane = p.lane, wm = p.wm, wn = p.wn;
-    const bool inside = m0 + kTile <= o.m;
-    const OutboxOf<T, kTile> outbox{lds};
-    Vec<T, 4> kept[sizeof(T) == 2 ? SUB : 1][sizeof(T) == 2 ? SUB : 1];
-#pragma unroll
-    for (int j = 0; j < SUB; ++j) {
-        const int64_t row = n0 + wn * kWave + j * 16 + (lane & 15);
-        const bool there = row < o.n;
-        const int64_t target = there ? load_index(targets, row, it) : -1;
-        const int64_t wanted64 = target - first_class - m0 - wm * kWave;
-        const int wanted = wanted64 >= 0 && wanted64 < kWave ? (int)wanted64 : -1;
-        const S u = there ? up[row] : (S)0, l = there ? lse[row] : (S)0;
-        const bool some = u != 0, any = __any(wanted >= 0);
-        T* g_at = g + row * g_pitch + m0 + wm * kWave + acc_row<T>(lane, 0);
-        T* gt_at = gt + (m0 + wm * kWave + acc_row<T>(lane, 0)) * gt_pitch + row;
-#pragma unroll
-        for (int i = 0; i < SUB; ++i) {
-            const int64_t cls = m0 + wm * kWave + i * 16;
-            S x[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = u * exp_of(acc[i][j][r] - l, T{});
-            if (any)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = i * 16 + acc_row<T>(lane, r) == wanted ? u * (exp_of(acc[i][j][r] - l, T{}) - (S)1) : x[r];
-            if (!inside)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = cls + acc_row<T>(lane, r) < o.m ? x[r] : (S)0;
-            Vec<T, 4> v;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v.v[r] = (T)(some ? x[r] : (S)0);   // rows without a target stay 0 whatever their logits are
-            if constexpr (sizeof(T) == 2) {
-                kept[i][j] = v;   // (of f16 and bf16)
-                outbox.put(wn * kWave + j * 16 + (lane & 15), wm * kWave + i * 16 + acc_row<T>(lane, 0), v);
-                continue;
-            }
-            // (g_pitch is a multiple of 16: the tile is in or out)
-            if (there && cls < g_pitch)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) g_at[i * 16 + acc_row<T>(0, r)] = v.v[r];
-            if (row < gt_pitch)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (inside || cls + acc_row<T>(lane, r) < o.m) gt_at[(i * 16 + acc_row<T>(0, r)) * gt_pitch] = v.v[r];
-        }
-    }
-    if constexpr (sizeof(T) == 2) {
-        outbox.send(g + n0 * g_pitch + m0, g_pitch, o.n - n0, g_pitch - m0);
-        // four lanes hold four classes of four rows, and each takes one class of the four rows
-#pragma unroll
-        for (int j = 0; j < SUB; ++j)
-#pragma unroll
-            for (int i = 0; i < SUB; ++i)
-                outbox.put(wm * kWave + i * 16 + acc_row<T>(lane, 0) + (lane & 3), wn * kWave + j * 16 + (lane & 12), turn(kept[i][j], lane));
-        outbox.send(gt + m0 * gt_pitch + n0, gt_pitch, o.m - m0, gt_pitch - n0);
-    }
-}
-
-// out[n][m] (pitch D) = the products times *unscale, rounded; or, with SUMS, sum[part][n][m] = the products over the part's steps, added to
-// what is there unless `first`.  parts: the steps are divided among this many workgroups per tile.
-template <typename T, int SUB, bool SUMS>
-__global__ __launch_bounds__(kThreads, 1) void product_kernel(Operands o, TileOrder order, typename Types<T>::Sum* sum, T* out, int64_t D, bool first,
-                                                              const typename Types<T>::Sum* unscale)
-{
-    using S = typename Types<T>::Sum;
-    using P = Product<T, SUB>;
-    constexpr int kTile = P::kTile, kWave = P::kWave;
-    extern __shared__ __align__(16) char lds[];
-    int64_t tile_m, tile_n;
-    const int part = tile_of(order, tile_m, tile_n);
-    const int64_t m0 = tile_m * kTile, n0 = tile_n * kTile;
-    if constexpr (SUMS) {
-        const int64_t from = o.steps * part / order.parts, to = o.steps * (part + 1) / order.parts;
-        o.a += from * kStepBytes;
-        o.b += from * kStepBytes;
-        o.steps = to - from;
-        sum += part * o.n * D;
-    }
-    P p;
-    p.run(o, m0, n0, lds);
-    auto& acc = p.acc;
-    const int lane = p.lane, wm = p.wm, wn = p.wn;
-    const S f = SUMS ? (S)1 : *unscale;
-    const OutboxOf<T, kTile> outbox{lds};
-#pragma unroll
-    for (int j = 0; j < SUB; ++j) {
-        const int64_t n = n0 + wn * kWave + j * 16 + (lane & 15);
-        if (n >= o.n) continue;
-#pragma unroll
-        for (int i = 0; i < SUB; ++i) {
-            const int col = wm * kWave + i * 16 + acc_row<T>(lane, 0);
-            const int64_t m = m0 + col, at = n * D + m;
-            constexpr int kApart = sizeof(T) == 8 ? 4 : 1;   // between the lane's four numbers
-            Vec<S, 4> x;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x.v[r] = acc[i][j][r];
-            if constexpr (SUMS) {
-                if (kApart == 1 && m + 3 < o.m) {
-                    if (!first) {
-                        const Vec<S, 4> before = load_vec<S, 4>(sum + at);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x.v[r] += before.v[r];
-                    }
-                    store_vec(sum + at, x);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (m + r * kApart < o.m) sum[at + r * kApart] = first ? x.v[r] : sum[at + r * kApart] + x.v[r];
-                }
-            } else {
-                Vec<T, 4> v;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v.v[r] = scaled<T>(x.v[r], f);
-                if constexpr (sizeof(T) == 2) outbox.put(wn * kWave + j * 16 + (lane & 15), col, v);
-                else if (kApart == 1 && m + 3 < o.m) store_vec(out + at, v);
-                else
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (m + r * kApart < o.m) out[at + r * kApart] = v.v[r];
+    Tiling best{};
+    double least = 1e300;
+    for (int sub = size == 8 ? 4 : 8; sub >= 2; sub /= 2) {
+        const int64_t tile = 32 * sub, tiles = ((m + tile - 1) / tile) * ((n + tile - 1) / tile);
+        const double busy = sub * sub * (size == 2 ? 43.0 : 270.0), fed = sub * 205.0 + 100.0;
+        for (int64_t parts = 1; parts <= most_parts && (parts == 1 || steps / parts >= 8); parts *= 2) {
+            const int64_t groups = tiles * parts, rounds = (groups + 255) / 256;
+            double step = std::max(busy, fed);
+            if (rounds == 1) step = std::max(step, 1000.0);
+            double cost = (double)rounds * ((double)((steps + parts - 1) / parts) * step + 6000.0);
+            if (parts > 1) cost += 8000.0 + 2.0 * (double)(parts * m * n * sum_size) / 2000.0;
+            if (cost < least) {
+                least = cost;
+                best = {sub, (int)parts};
             }
         }
     }
-    if constexpr (sizeof(T) == 2 && !SUMS) outbox.send(out + n0 * D + m0, D, o.n - n0, o.m - m0);
-}
-
-// out = the parts' sums in their order, times *unscale, rounded.
-template <typename T>
-__global__ __launch_bounds__(256) void finish_kernel(const typename Types<T>::Sum* sum, int parts, int64_t entries, const typename Types<T>::Sum* unscale,
-                                                     T* out)
-{
-    using S = typename Types<T>::Sum;
-    constexpr int E = 16 / sizeof(S);
-    const S f = *unscale;
-    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E; i < entries; i += (int64_t)gridDim.x * 256 * E) {
-        const int n = entries - i < E ? (int)(entries - i) : E;
-        Vec<S, E> x = n == E ? load_vec<S, E>(sum + i) : load_some<S, E>(sum + i, n);
-        for (int k = 1; k < parts; ++k) {
-            const S* from = sum + k * entries + i;
-            const Vec<S, E> y = n == E ? load_vec<S, E>(from) : load_some<S, E>(from, n);
-#pragma unroll
-            for (int e = 0; e < E; ++e) x.v[e] += y.v[e];
-        }
-        Vec<T, E> v;
-#pragma unroll
-        for (int e = 0; e < E; ++e) v.v[e] = scaled<T>(x.v[e], f);
-        if (n == E) store_vec(out + i, v);
-        else store_some(out + i, v, n);
-    }
-}
-
-// ------------------------------------------------------------------------------------------------ copies
-// dst[rows][pitch] = src[rows][cols], zeros behind the columns.
-template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(const T* src, T* dst, int64_t rows, int64_t cols, int64_t pitch)
-{
-    constexpr int E = kPer16<T>;
-    const int64_t per_row = pitch / E, items = rows * per_row;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / per_row, col = (i - row * per_row) * E;
-        const int64_t left = cols - col;
-        const Vec<T, E> v = left >= E ? load_vec<T, E>(src + row * cols + col) : load_some<T, E>(src + row * cols + col, (int)(left > 0 ? left : 0));
-        store_vec(dst + row * pitch + col, v);
-    }
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void zero_kernel(T* p, int64_t n)
-{
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = T(0);
-}
-
-// dst[cols][pitch] = src[rows][cols] transposed, zeros behind the rows.  targets not null: rows without one are zeros, whatever they hold.
-// A workgroup turns 64 x 64 entries (32 x 64 of double), moved as 16 bytes either way.
-template <typename T>
-constexpr int kTurnCols = sizeof(T) == 8 ? 32 : 64;
-template <typename T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* src, T* dst, int64_t rows, int64_t cols, int64_t pitch, const void* targets,
-                                                        int it, int64_t V)
-{
-    constexpr int R = 64, C = kTurnCols<T>, E = kPer16<T>, kPad = 4 / sizeof(T) ? 4 / sizeof(T) : 1;
-    __shared__ T tile[C][R + kPad];   // (an odd number of words from column to column, or of double words)
-    const int64_t r0 = (int64_t)blockIdx.x * R, c0 = (int64_t)blockIdx.y * C;
-    for (int i = threadIdx.x; i < R * C / E; i += 256) {
-        const int row = i / (C / E), col = i % (C / E) * E;
-        const int64_t r = r0 + row, left = cols - c0 - col;
-        bool there = r < rows && left > 0;
-        if (there && targets) {
-            const int64_t t = load_index(targets, r, it);
-            there = t >= 0 && t < V;
-        }
-        Vec<T, E> v;
-        const T* from = src + r * cols + c0 + col;
-        if (there && left >= E) v = load_vec<T, E>(from);
-        else v = load_some<T, E>(from, there ? (int)left : 0);
-#pragma unroll
-        for (int e = 0; e < E; ++e) tile[col + e][row] = v.v[e];
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < R * C / E; i += 256) {
-        const int col = i / (R / E), row = i % (R / E) * E;
-        // (the pitch is a multiple of 16 bytes)
-        if (c0 + col >= cols || r0 + row >= pitch) continue;
-        Vec<T, E> v;
-#pragma unroll
-        for (int e = 0; e < E; ++e) v.v[e] = tile[col][row + e];
-        store_vec(dst + (c0 + col) * pitch + r0 + row, v);
-    }
-}
-
-// ------------------------------------------------------------------------------------------------ rows
-// Joins the tiles' maxima and sums of a piece with the running ones; after the last piece lse and the row's loss.
-// A workgroup takes 64 rows, 16 threads each over the tiles.
-template <typename T>
-__global__ __launch_bounds__(1024) void join_kernel(const typename Types<T>::Sum* part_max, const typename Types<T>::Sum* part_sum, int64_t tiles,
-                                                    int64_t rows, bool first, bool last, typename Types<T>::Sum* run_max,
-                                                    typename Types<T>::Sum* run_sum, const typename Types<T>::Sum* hit, const void* targets, int it,
-                                                    int64_t V, typename Types<T>::Sum* lse, typename Types<T>::Sum* losses)
-{
-    using S = typename Types<T>::Sum;
-    __shared__ S tops[16][64], sums[16][64];
-    const int lane = threadIdx.x & 63, seg = threadIdx.x >> 6;
-    const int64_t row = (int64_t)blockIdx.x * 64 + lane;
-    S top = lowest<S>(), sum = 0;
-    auto add = [&](S t, S s) {
-        const S m = larger(t, top);
-        sum = sum * exp_below<T>(top, m) + s * exp_below<T>(t, m);
-        top = m;
-    };
-    if (row < rows) {
-        if (seg == 0 && !first) add(run_max[row], run_sum[row]);
-        for (int64_t i = seg; i < tiles; i += 16) add(part_max[i * rows + row], part_sum[i * rows + row]);
-    }
-    tops[seg][lane] = top;
-    sums[seg][lane] = sum;
-    __syncthreads();
-    if (seg != 0 || row >= rows) return;
-    for (int i = 1; i < 16; ++i) add(tops[i][lane], sums[i][lane]);
-    if (!last) {
-        run_max[row] = top;
-        run_sum[row] = sum;
-        return;
-    }
-    const S l = top + log_of(sum);
-    const int64_t target = load_index(targets, row, it);
-    lse[row] = l;
-    losses[row] = target >= 0 && target < V ? l - hit[row] : (S)0;
-}
-
-// The rows with a target and, unless reduction is ST_NONE, the sum or mean of their losses.  One workgroup.
-template <typename S>
-__global__ __launch_bounds__(1024) void reduce_kernel(const S* losses, const void* targets, int it, int64_t rows, int64_t V, int reduction, S* loss,
-                                                      double* count)
-{
-    __shared__ double scratch[32];
-    double sum = 0, n = 0;
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
-        const int64_t t = load_index(targets, i, it);
-        if (t >= 0 && t < V) {
-            n += 1;
-            if (reduction != ST_NONE) sum += (double)losses[i];
-        }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o /= 2) {
-        sum += __shfl_xor(sum, o);
-        n += __shfl_xor(n, o);
-    }
-    if ((threadIdx.x & 63) == 0) {
-        scratch[threadIdx.x >> 6] = sum;
-        scratch[16 + (threadIdx.x >> 6)] = n;
-    }
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    sum = n = 0;
-    for (int i = 0; i < 16; ++i) {
-        sum += scratch[i];
-        n += scratch[16 + i];
-    }
-    *count = n;
-    if (reduction == ST_SUM) *loss = (S)sum;
-    if (reduction == ST_MEAN) *loss = (S)(n > 0 ? sum / n : 0.0);
-}
-
-// Every row's upstream gradient over the largest of them, and that one: scaling[0].  The logits' gradients are rounded to T, and a common
-// factor that T does not hold (one over the number of rows) would put all of them off by the same part of a step.  f16 takes 2^14 times as
-// much, or small probabilities would be subnormal.  One workgroup.
-template <typename T>
-__global__ __launch_bounds__(1024) void upstream_kernel(const typename Types<T>::Sum* grad, const void* targets, int it, int64_t rows, int64_t V,
-                                                        int reduction, const double* count, typename Types<T>::Sum* up,
-                                                        typename Types<T>::Sum* scaling)
-{
-    using S = typename Types<T>::Sum;
-    constexpr S kRange = std::is_same_v<T, f16> ? (S)16384 : (S)1;
-    __shared__ S tops[16];
-    auto has = [&](int64_t i) {
-        const int64_t t = load_index(targets, i, it);
-        return t >= 0 && t < V;
-    };
-    S top = 1;
-    if (reduction == ST_NONE) {
-        top = 0;
-        for (int64_t i = threadIdx.x; i < rows; i += 1024) {
-            const S a = has(i) ? (grad[i] < 0 ? -grad[i] : grad[i]) : (S)0;
-            top = a > top ? a : top;
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o /= 2) {
-            const S a = __shfl_xor(top, o);
-            top = a > top ? a : top;
-        }
-        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-        __syncthreads();
-        for (int i = 0; i < 16; ++i) top = tops[i] > top ? tops[i] : top;
-        if (!(top > 0 && top < (S)__builtin_inf())) top = 1;
-    }
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) up[i] = !has(i) ? (S)0 : reduction == ST_NONE ? grad[i] / top * kRange : kRange;
-    if (threadIdx.x == 0) {
-        const S all = reduction == ST_MEAN ? (S)((double)grad[0] / *count) : reduction == ST_SUM ? grad[0] : top;
-        *scaling = all / kRange;
-    }
-}
-
-unsigned blocks_for(int64_t items) { return (unsigned)((items + 255) / 256 < 16384 ? (items + 255) / 256 : 16384); }
-
-#define ST_TRY(call)                               \
-    do {                                           \
-        (call);                                    \
-        const hipError_t err_ = hipGetLastError(); \
-        if (err_ != hipSuccess) return err_;       \
-    } while (0)
-
-// A matrix with rows in whole steps: the caller's, or a copy.
-template <typename T>
-hipError_t in_steps(const T* src, int64_t rows, int64_t cols, int64_t pitch, void* copy, const T** out, hipStream_t st)
-{
-    *out = src;
-    if (cols == pitch && reinterpret_cast<uintptr_t>(src) % 16 == 0) return hipSuccess;
-    *out = static_cast<const T*>(copy);
-    ST_TRY((pack_kernel<T><<<blocks_for(rows * (pitch / kPer16<T>)), 256, 0, st>>>(src, static_cast<T*>(copy), rows, cols, pitch)));
-    return hipSuccess;
-}
-
-template <typename T>
-Operands operands(const T* a, int64_t a_cols, int64_t m, const T* b, int64_t b_cols, int64_t n, int64_t k)
-{
-    return {reinterpret_cast<const char*>(a), reinterpret_cast<const char*>(b), a_cols * (int64_t)sizeof(T), b_cols * (int64_t)sizeof(T), m, n,
-            k * (int64_t)sizeof(T) / kStepBytes};
-}
-template <typename T>
-constexpr int kSub = sizeof(T) == 8 ? 4 : 8;
-template <typename T>
-TileOrder tiles_of(int64_t m, int64_t n)
-{
-    constexpr int kTile = Product<T, kSub<T>>::kTile;
-    static_assert(kTile >= kTileLeast && kTileRows % kTile == 0);
-    return {(uint32_t)((m + kTile - 1) / kTile), (uint32_t)((n + kTile - 1) / kTile)};
-}
-// (more than 64 KiB of LDS have to be asked for, once per device)
-template <typename T, typename K, typename... Args>
-hipError_t launch_product(K kernel, const TileOrder& t, hipStream_t st, const Args&... args)
-{
-    constexpr size_t lds = Product<T, kSub<T>>::kLds;
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-    kernel<<<t.tiles_m * t.tiles_n * t.parts, kThreads, lds, st>>>(args...);
-    return hipGetLastError();
-}
-
-template <typename T>
-hipError_t run_fwd(const EntropyPlan& p, const T* h, const T* w, const void* targets, void* loss, void* lse, double* rows, int reduction, int it,
-                   unsigned char* ws, hipStream_t st)
-{
-    using S = typename Types<T>::Sum;
-    if (p.T == 0) {
-        ST_TRY((reduce_kernel<S><<<1, 1024, 0, st>>>(nullptr, nullptr, it, 0, p.V, reduction, static_cast<S*>(loss), rows)));
-        return hipSuccess;
-    }
-    const T* hs;
-    hipError_t e = in_steps(h, p.T, p.D, p.Dp, ws + p.off_h, &hs, st);
-    if (e != hipSuccess) return e;
-    S *run_max = reinterpret_cast<S*>(ws + p.off_max), *run_sum = reinterpret_cast<S*>(ws + p.off_sum), *hit = reinterpret_cast<S*>(ws + p.off_hit);
-    const int64_t most = p.piece / kTileLeast;
-    S *part_max = reinterpret_cast<S*>(ws + p.off_part), *part_sum = part_max + most * p.T;
-    // (the running maxima are dead where the losses of the rows are written: a thread reads its own first)
-    S* losses = reduction == ST_NONE ? static_cast<S*>(loss) : run_max;
-    for (int64_t i = 0; i < p.pieces; ++i) {
-        const int64_t first = i * p.piece, n = p.V - first < p.piece ? p.V - first : p.piece;
-        const T* wsrc;
-        if ((e = in_steps(w + first * p.D, n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
-        const Operands o = operands(wsrc, p.Dp, n, hs, p.Dp, p.T, p.Dp);
-        const TileOrder t = tiles_of<T>(n, p.T);
-        if ((e = launch_product<T>(stats_kernel<T, kSub<T>>, t, st, o, t, targets, it, first, p.V, part_max, part_sum, hit)) != hipSuccess) return e;
-        ST_TRY((join_kernel<T><<<(unsigned)((p.T + 63) / 64), 1024, 0, st>>>(part_max, part_sum, t.tiles_m, p.T, i == 0, i + 1 == p.pieces, run_max,
-                                                                            run_sum, hit, targets, it, p.V, static_cast<S*>(lse), losses)));
-    }
-    ST_TRY((reduce_kernel<S><<<1, 1024, 0, st>>>(losses, targets, it, p.T, p.V, reduction, static_cast<S*>(loss), rows)));
-    return hipSuccess;
-}
-
-template <typename T>
-hipError_t run_bwd(const EntropyPlan& p, const T* h, const T* w, const void* targets, const void* lse, const double* rows, const void* grad,
-                   T* grad_h, T* grad_w, int reduction, int it, unsigned char* ws, hipStream_t st)
-{
-    using S = typename Types<T>::Sum;
-    if (p.T == 0) {
-        if (grad_w) ST_TRY((zero_kernel<T><<<blocks_for(p.V * p.D), 256, 0, st>>>(grad_w, p.V * p.D)));
-        return hipSuccess;
-    }
-    S *up = reinterpret_cast<S*>(ws + p.off_up), *scaling = up + p.T, *dh = reinterpret_cast<S*>(ws + p.off_dh);
-    T *ht = reinterpret_cast<T*>(ws + p.off_ht), *wt = reinterpret_cast<T*>(ws + p.off_wt);
-    T *g = reinterpret_cast<T*>(ws + p.off_g), *gt = reinterpret_cast<T*>(ws + p.off_gt);
-    ST_TRY((upstream_kernel<T><<<1, 1024, 0, st>>>(static_cast<const S*>(grad), targets, it, p.T, p.V, reduction, rows, up, scaling)));
-    const T* hs;
-    hipError_t e = in_steps(h, p.T, p.D, p.Dp, ws + p.off_h, &hs, st);
-    if (e != hipSuccess) return e;
-    auto turn = [&](const T* src, T* dst, int64_t r, int64_t pitch, const void* only) -> hipError_t {
-        ST_TRY((transpose_kernel<T><<<dim3((unsigned)((pitch + 63) / 64), (unsigned)((p.D + kTurnCols<T> - 1) / kTurnCols<T>)), 256, 0, st>>>(src, dst, r, p.D, pitch, only, it,
-                                                                                                                  p.V)));
-        return hipSuccess;
-    };
-    if (grad_w && (e = turn(h, ht, p.T, p.Tp, targets)) != hipSuccess) return e;
-    for (int64_t i = 0; i < p.pieces; ++i) {
-        const int64_t first = i * p.piece, n = p.V - first < p.piece ? p.V - first : p.piece;
-        const int64_t per = kStepBytes / (int64_t)sizeof(T), np = (n + per - 1) / per * per;
-        const T* wsrc;
-        if ((e = in_steps(w + first * p.D, n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
-        const Operands logits = operands(wsrc, p.Dp, n, hs, p.Dp, p.T, p.Dp);
-        TileOrder t = tiles_of<T>(n, p.T);
-        if ((e = launch_product<T>(grads_kernel<T, kSub<T>>, t, st, logits, t, targets, it, first, static_cast<const S*>(lse), up, g, np, gt, p.Tp)) !=
-            hipSuccess)
-            return e;
-        if (grad_h) {
-            if ((e = turn(w + first * p.D, wt, n, np, nullptr)) != hipSuccess) return e;
-            const Operands o = operands(wt, np, p.D, g, np, p.T, np);
-            t = tiles_of<T>(p.D, p.T);
-            t.parts = (uint32_t)p.parts;
-            if (p.sums) e = launch_product<T>(product_kernel<T, kSub<T>, true>, t, st, o, t, dh, (T*)nullptr, p.D, i == 0, scaling);
-            else e = launch_product<T>(product_kernel<T, kSub<T>, false>, t, st, o, t, dh, grad_h, p.D, true, scaling);
-            if (e != hipSuccess) return e;
-        }
-        if (grad_w) {
-            const Operands o = operands(ht, p.Tp, p.D, gt, p.Tp, n, p.Tp);
-            t = tiles_of<T>(p.D, n);
-            if ((e = launch_product<T>(product_kernel<T, kSub<T>, false>, t, st, o, t, (S*)nullptr, grad_w + first * p.D, p.D, true, scaling)) != hipSuccess)
-                return e;
-        }
-    }
-    if (grad_h && p.sums) ST_TRY((finish_kernel<T><<<blocks_for((p.T * p.D + 3) / 4), 256, 0, st>>>(dh, (int)p.parts, p.T * p.D, scaling, grad_h)));
-    return hipSuccess;
+    return best;
 }
 
 template <typename F>
@@ -957,32 +69,37 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
     auto lay = [&](int64_t piece) {
         p.piece = piece;
         p.pieces = (V + piece - 1) / piece;
+        const int64_t classes = std::min(piece, V);
         size_t at = 0;
         auto take = [&](int64_t entries, int size) {
             const size_t here = at;
             at += round_up((size_t)entries * size, 256);
             return here;
         };
-        p.off_h = take(T * p.Dp, p.size);
-        p.off_w = take(piece * p.Dp, p.size);
+        p.few = !backward && T <= 16;
+        // (where the logits are few their parts are small; the least workspace has no place for parts)
+        p.logits = choose_tiling(p.size, classes, T, p.Dp / per, p.few || least || T > 65535 || classes * T > (1 << 22) ? 1 : 16, p.sum_size);
+        p.off_h = take(p.few ? 0 : T * p.Dp, p.size);
+        p.off_w = take(p.few ? 0 : piece * p.Dp, p.size);
+        p.off_z = take(p.logits.parts > 1 ? p.logits.parts * T * classes : 0, p.sum_size);
         if (!backward) {
+            p.part_classes = p.few ? 64 : p.logits.parts > 1 ? 256 : 32 * p.logits.sub;
             p.off_max = take(T, p.sum_size);
             p.off_sum = take(T, p.sum_size);
             p.off_hit = take(T, p.sum_size);
-            p.off_part = take(2 * T * (piece / kTileLeast), p.sum_size);
+            p.off_part = take(2 * T * ((piece + p.part_classes - 1) / p.part_classes), p.sum_size);
         } else {
+            p.by_h = choose_tiling(p.size, D, T, (classes + per - 1) / per, least ? 1 : 64, p.sum_size);
+            p.by_w = choose_tiling(p.size, D, classes, p.Tp / per, 1, p.sum_size);
+            p.sums = p.pieces > 1 || p.by_h.parts > 1;
             p.off_up = take(T + 2, p.sum_size);
             p.off_ht = take(D * p.Tp, p.size);
             p.off_wt = take(D * piece, p.size);
             p.off_g = take(T * piece, p.size);
             p.off_gt = take(piece * p.Tp, p.size);
-            // few tiles of grad_h: several workgroups per tile, as long as each has 16 steps
-            const int64_t tile = p.size == 8 ? 128 : 256, tiles = (T + tile - 1) / tile * ((D + tile - 1) / tile);
-            p.parts = std::max<int64_t>(1, std::min<int64_t>(256 / std::max<int64_t>(tiles, 1), std::min(piece, V) / per / 16));
-            p.sums = p.pieces > 1 || p.parts > 1;
-            p.off_dh = take(p.sums ? p.parts * T * D : 0, p.sum_size);
+            p.off_dh = take(p.sums ? p.by_h.parts * T * D : 0, p.sum_size);
         }
-        p.total = at;
+        p.total = std::max<size_t>(at, 256);
     };
     const int64_t all = (V + kTileRows - 1) / kTileRows * kTileRows;
     if (least) {
@@ -991,16 +108,23 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
     }
     // Pieces of at most 1 GiB of what a class takes, and of those the size for which the compute units' rounds of tiles, over all pieces and products, are
     // fewest: 8192 rows and 4096 channels in pieces of 10240 classes have 640 tiles of grad_w, two and a half rounds that take three.
-    const int64_t each = backward ? 2 * p.Tp * p.size + 2 * p.Dp * p.size : p.Dp * p.size + 2 * T * p.sum_size / kTileLeast + 1;
+    const int64_t each = backward ? 2 * p.Tp * p.size + 2 * p.Dp * p.size : (T <= 16 ? 0 : p.Dp * p.size) + 2 * T * p.sum_size / 64 + 1;
     int64_t most = ((int64_t)1 << 30) / each / kTileRows;
     if (most < 1) most = 1;
     if (most > (1 << 14)) most = 1 << 14;   // (tiles of a piece are a grid's second index)
+    if (most > all / kTileRows) most = all / kTileRows;
     auto fits = [&](int64_t rows) {
         lay(rows * kTileRows);
         return ws_bytes == 0 || p.total <= ws_bytes;
     };
-    while (most > 1 && !fits(most)) most -= (most + 15) / 16;
-    if (most >= all / kTileRows) most = all / kTileRows;
+    if (!fits(most)) {   // the largest that does, between one that does and one that does not
+        int64_t yes = 1, no = most;
+        while (no - yes > 1) {
+            const int64_t mid = (yes + no) / 2;
+            (fits(mid) ? yes : no) = mid;
+        }
+        most = yes;
+    }
     int64_t best = most;
     if (backward && most < all / kTileRows) {
         const int64_t tile = p.size == 8 ? 128 : 256, units = 256, per_row = kTileRows / tile;
@@ -1011,7 +135,7 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
             // a round of logits takes D steps, of grad_w T and of grad_h the piece's classes
             const double one = rounds(rows * per_row * tt) * (double)D + rounds(rows * per_row * td) * (double)T + rounds(tt * td) * (double)(rows * kTileRows);
             const double cost = one * (double)((all / kTileRows + rows - 1) / rows);
-            if (cost < least_cost * 0.999) {
+            if (cost < least_cost * 0.999 && fits(rows)) {
                 least_cost = cost;
                 best = rows;
             }
@@ -1020,8 +144,9 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
     if (!backward) {   // of about the same size
         const int64_t count = (all / kTileRows + most - 1) / most;
         best = (all / kTileRows + count - 1) / count;
+        if (!fits(best)) best = most;
     }
-    lay(best * kTileRows);
+    if (!fits(best)) return entropy_plan(backward, T, V, D, dt, true, 0);   // (the smallest pieces without parts: what the least workspace holds)
     return p;
 }
 
@@ -1030,7 +155,7 @@ hipError_t entropy_fwd(const EntropyPlan& p, const void* h, const void* w, const
 {
     return by_type(dt, [&](auto type) {
         using T = decltype(type);
-        return run_fwd<T>(p, static_cast<const T*>(h), static_cast<const T*>(w), targets, loss, lse, rows, reduction, it,
+        return entropy_run_fwd<T>(p, static_cast<const T*>(h), static_cast<const T*>(w), targets, loss, lse, rows, reduction, it,
                           static_cast<unsigned char*>(ws), st);
     });
 }
@@ -1040,7 +165,7 @@ hipError_t entropy_bwd(const EntropyPlan& p, const void* h, const void* w, const
 {
     return by_type(dt, [&](auto type) {
         using T = decltype(type);
-        return run_bwd<T>(p, static_cast<const T*>(h), static_cast<const T*>(w), targets, lse, rows, grad, static_cast<T*>(grad_h),
+        return entropy_run_bwd<T>(p, static_cast<const T*>(h), static_cast<const T*>(w), targets, lse, rows, grad, static_cast<T*>(grad_h),
                           static_cast<T*>(grad_w), reduction, it, static_cast<unsigned char*>(ws), st);
     });
 }

@@ -36,15 +36,20 @@ hipError_t embed_bwd(const EmbedPlan& p, const void* tokens, const void* grad_ou
 // the caller's arrays where they have that form, copies elsewhere.
 constexpr int kStepBytes = 128;   // of a row, taken at a time by the products
 constexpr int kTileRows = 256;    // pieces of the classes are multiples of this
-constexpr int kTileLeast = 128;   // classes and rows per workgroup of the products: this or twice as many
+struct Tiling {
+    int sub = 2, parts = 1;       // 16 x 16 tiles on a side of a wave's, and workgroups that divide a tile's steps
+};
 struct EntropyPlan {
     int64_t T, V, D;
     int size, sum_size;        // bytes of an element and of a sum
     int64_t Dp, Tp;            // D and T in whole steps
     int64_t piece, pieces;     // classes per piece (a multiple of kTileRows)
-    int64_t parts;             // backward: workgroups per tile of grad_h, which divide a piece's classes
-    bool sums;                 // ... and whether grad_h is summed over pieces or parts
+    bool few;                  // forward, of at most 16 rows: w is read straight from memory
+    int64_t part_classes;      // ... classes whose maximum and sum are formed together
+    Tiling logits, by_h, by_w; // the products of the logits and of both gradients
+    bool sums;                 // whether grad_h is summed over pieces or parts
     size_t off_h, off_w;       // copies of h and of a piece of w with rows of Dp (used where the caller's do not fit)
+    size_t off_z;              // the logits as sums over parts, where they are divided
     size_t off_max, off_sum, off_hit;   // forward: running maximum and sum, and the target's logit, of every row
     size_t off_part;           // ... and those of the piece's tiles
     size_t off_up;             // backward: every row's upstream gradient (and behind them the scaling, two numbers)
