@@ -267,7 +267,9 @@ def embed(tokens, table, scale=1.0):
     """scale * table[tokens], [..., D] for integer device tensors tokens[...] and table[V, D]: sequences of symbols [B, L] as the paths
     [B, L, D] that the calls above take; differentiable in table (the rows of a symbol are summed in a fixed order).  A token
     outside 0 .. V - 1 (padding) gives zeros and takes no part in the gradient."""
-    return _Embed.apply(tokens, table, float(scale))
+    scale = float(scale)
+    out = _native.embed(tokens, table, scale)
+    return _Embed.apply(tokens, table, scale) if out is None else out
 
 
 def linear_cross_entropy(h, weight, targets, reduction="mean"):
@@ -275,6 +277,10 @@ def linear_cross_entropy(h, weight, targets, reduction="mean"):
     are none), the sum, or with "none" every row's; differentiable in h and weight.  The logits of all classes never exist at
     once, forward or backward.  A row whose target is outside 0 .. V - 1 has none: its loss and its gradient are 0, and what it holds
     reaches nothing.  float32 (float64 for float64 arrays)."""
+    if isinstance(reduction, str):
+        loss = _native.entropy(h, weight, targets, reduction)
+        if loss is not None:
+            return loss
     if h.shape[:-1] != targets.shape:
         raise ValueError("h[..., D] and targets[...] expected, got %s and %s" % (tuple(h.shape), tuple(targets.shape)))
     loss = _LinearCrossEntropy.apply(h.reshape(-1, h.shape[-1]), weight, targets.reshape(-1), reduction)

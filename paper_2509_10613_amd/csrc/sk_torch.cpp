@@ -11,12 +11,14 @@
 // above the given limit (their accounting lives there), and whatever the library refuses (the classes then raise).
 #include <ATen/ATen.h>
 #include <ATen/SavedTensorHooks.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/edge.h>
 #include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/saved_variable.h>
@@ -26,6 +28,7 @@
 
 #include <array>
 #include <atomic>
+#include <cmath>
 #include <cstring>
 #include <limits>
 #include <memory>
@@ -34,6 +37,7 @@
 
 #include "sigkernel.h"
 #include "signature.h"
+#include "sigtrain.h"
 
 namespace {
 
@@ -299,6 +303,126 @@ struct SignatureNode : public Node {
     }
 };
 
+// ---------------------------------------------------------------- both ends of a model (sigtrain.h)
+bool st_type(const Tensor& t, st_dtype& dt)
+{
+    switch (t.scalar_type()) {
+    case at::kDouble: dt = ST_F64; return true;
+    case at::kFloat: dt = ST_F32; return true;
+    case at::kBFloat16: dt = ST_BF16; return true;
+    case at::kHalf: dt = ST_F16; return true;
+    default: return false;
+    }
+}
+st_itype st_index(const Tensor& t) { return t.scalar_type() == at::kInt ? ST_I32 : ST_I64; }
+
+// The gradients of a backward call that is not itself differentiable: what asks for more meets an error, as with once_differentiable.
+variable_list once(variable_list&& out, const variable_list& grads)
+{
+    if (!at::GradMode::is_enabled() || !grads[0].defined() || !grads[0].requires_grad()) return std::move(out);
+    variable_list some;
+    for (const Tensor& t : out)
+        if (t.defined()) some.push_back(t.detach().requires_grad_());
+    const auto node = std::shared_ptr<Node>(
+        new torch::autograd::DelayedError("trying to differentiate twice a function that was marked with @once_differentiable", (int64_t)some.size()),
+        torch::autograd::deleteNode);
+    variable_list marked = (*node)(std::move(some));
+    size_t at = 0;
+    for (Tensor& t : out)
+        if (t.defined()) t = marked[at++];
+    return std::move(out);
+}
+
+struct EmbedNode : public Node {
+    SavedVariable tokens_;
+    int64_t V = 0;
+    double scale = 1;
+    size_t need = 0;
+    std::vector<int64_t> token_sizes, out_sizes;
+    at::TensorOptions options, token_options;
+    std::string name() const override { return "EmbedBackward"; }
+    void release_variables() override
+    {
+        const Lock lock(mutex_);
+        tokens_.reset_data();
+    }
+    variable_list apply(variable_list&& grads) override
+    {
+        Tensor tokens, table;
+        {
+            const Lock lock(mutex_);
+            tokens = tokens_.unpack();
+        }
+        {
+            at::NoGradGuard no_grad;
+            const c10::DeviceGuard device(options.device());
+            const Tensor g = grads[0].defined() ? grads[0].contiguous() : at::zeros(out_sizes, options);
+            expect(tokens, "the tokens", token_sizes, token_options);
+            expect(g, "the upstream gradient", out_sizes, options);
+            const int64_t D = out_sizes.back();
+            st_dtype dt = ST_F32;
+            st_type(g, dt);
+            table = at::empty({V, D}, options);
+            const Tensor w = bytes(need, g);
+            check(sigtrain_embed_bwd(tokens.data_ptr(), g.data_ptr(), table.data_ptr(), tokens.numel(), V, D, scale, st_index(tokens), dt,
+                                     w.data_ptr(), (size_t)w.numel(), current_stream()));
+        }
+        return once({table}, grads);
+    }
+};
+
+struct EntropyNode : public Node {
+    SavedVariable h_, w_, targets_;
+    Tensor lse, rows;
+    int reduction = ST_MEAN;
+    bool want_h = false, want_w = false;
+    size_t need = 0;
+    std::vector<int64_t> h_sizes, h_shape, w_sizes, target_sizes, out_sizes;   // h_shape: as the caller's
+    at::TensorOptions options, out_options, target_options;
+    std::string name() const override { return "LinearCrossEntropyBackward"; }
+    void release_variables() override
+    {
+        const Lock lock(mutex_);
+        h_.reset_data();
+        w_.reset_data();
+        targets_.reset_data();
+        lse.reset();
+        rows.reset();
+    }
+    variable_list apply(variable_list&& grads) override
+    {
+        variable_list out(2);
+        if (!want_h && !want_w) return out;
+        Tensor h, w, targets, l, n;
+        {
+            const Lock lock(mutex_);
+            h = h_.unpack();
+            w = w_.unpack();
+            targets = targets_.unpack();
+            l = lse;
+            n = rows;
+        }
+        {
+            at::NoGradGuard no_grad;
+            const c10::DeviceGuard device(options.device());
+            const Tensor g = grads[0].defined() ? grads[0].contiguous() : at::zeros(out_sizes, out_options);
+            expect(h, "h", h_sizes, options);
+            expect(w, "the read-out", w_sizes, options);
+            expect(targets, "the targets", target_sizes, target_options);
+            expect(g, "the upstream gradient", out_sizes, out_options);
+            st_dtype dt = ST_F32;
+            st_type(h, dt);
+            const int64_t T = h_sizes[0], D = h_sizes[1], V = w_sizes[0];
+            if (want_h) out[0] = at::empty(h_shape, options);
+            if (want_w) out[1] = at::empty(w_sizes, options);
+            const Tensor ws = workspace(need, h, [&] { return sigtrain_entropy_workspace_bytes(1, T, V, D, dt, 1); });
+            check(sigtrain_entropy_bwd(h.data_ptr(), w.data_ptr(), targets.data_ptr(), l.data_ptr(), n.data_ptr<double>(), g.data_ptr(), ptr(out[0]),
+                                       ptr(out[1]), T, V, D, reduction, st_index(targets), dt, ws.data_ptr(), (size_t)ws.numel(), current_stream()));
+        }
+        return once(std::move(out), grads);
+    }
+};
+
 template <class T>
 std::shared_ptr<T> make_node()
 {
@@ -530,6 +654,121 @@ py::object signature(py::object xo, py::object No, py::object fl)
     return wrap(out);
 }
 
+// a device tensor of one of the types of sigtrain.h, without forward gradients; symbols and targets: whole numbers
+bool plain_st(const py::object& o, Tensor& t, st_dtype& dt)
+{
+    if (!THPVariable_Check(o.ptr())) return false;
+    t = THPVariable_Unpack(o.ptr());
+    return t.is_cuda() && t.layout() == at::kStrided && st_type(t, dt) && !t.key_set().has(c10::DispatchKey::Python) && !t._fw_grad(0).defined() &&
+           !t.is_conj() && !t.is_neg();
+}
+bool plain_index(const py::object& o, const Tensor& beside, Tensor& t)
+{
+    if (!THPVariable_Check(o.ptr())) return false;
+    t = THPVariable_Unpack(o.ptr());
+    return t.is_cuda() && t.layout() == at::kStrided && (t.scalar_type() == at::kLong || t.scalar_type() == at::kInt) &&
+           !t.key_set().has(c10::DispatchKey::Python) && t.device() == beside.device();
+}
+
+py::object embed(py::object to, py::object wo, double scale)
+{
+    Tensor tokens0, table0, out;
+    st_dtype dt;
+    if (transformed() || !plain_st(wo, table0, dt) || table0.dim() != 2 || !plain_index(to, table0, tokens0) || !std::isfinite(scale)) return py::none();
+    {
+        py::gil_scoped_release release;
+        const bool grad = at::GradMode::is_enabled() && table0.requires_grad();
+        const c10::DeviceGuard device(table0.device());
+        const int64_t V = table0.size(0), D = table0.size(1), n = tokens0.numel();
+        Tensor tokens;
+        {
+            at::NoGradGuard no_grad;
+            tokens = tokens0.contiguous();
+            const Tensor table = table0.contiguous();
+            std::vector<int64_t> sizes = tokens0.sizes().vec();
+            sizes.push_back(D);
+            out = at::empty(sizes, table.options());
+            if (sigtrain_embed_fwd(tokens.data_ptr(), table.data_ptr(), out.data_ptr(), n, V, D, scale, st_index(tokens), dt, current_stream()) != SK_OK)
+                out.reset();
+        }
+        if (out.defined() && grad) {
+            const ShapeKey key{{32 | (int64_t)dt << 8, n, V, D, 0, 0, 0, 0}};
+            auto node = make_node<EmbedNode>();
+            node->set_next_edges(torch::autograd::collect_next_edges(table0));
+            node->tokens_ = SavedVariable(tokens, false);
+            node->V = V;
+            node->scale = scale;
+            node->need = need_of(key, [&] { return Need{0, 0, sigtrain_embed_bwd_workspace_bytes(n, V, D, dt), 0, 0}; }).backward;
+            node->token_sizes = tokens.sizes().vec();
+            node->out_sizes = out.sizes().vec();
+            node->options = out.options();
+            node->token_options = tokens.options();
+            torch::autograd::set_history(out, node);
+        }
+    }
+    return wrap(out);
+}
+
+py::object entropy(py::object ho, py::object wo, py::object to, const std::string& how)
+{
+    Tensor h0, w0, targets0, loss;
+    st_dtype dt, dtw;
+    const int reduction = how == "none" ? ST_NONE : how == "mean" ? ST_MEAN : how == "sum" ? ST_SUM : -1;
+    if (transformed() || reduction < 0 || !plain_st(ho, h0, dt) || !plain_st(wo, w0, dtw) || dt != dtw || h0.device() != w0.device() ||
+        !plain_index(to, h0, targets0) || h0.dim() < 1 || w0.dim() != 2 || h0.size(-1) != w0.size(1) || h0.size(-1) == 0 ||
+        h0.sizes().slice(0, h0.dim() - 1) != targets0.sizes())
+        return py::none();
+    {
+        py::gil_scoped_release release;
+        const bool grad = at::GradMode::is_enabled() && (h0.requires_grad() || w0.requires_grad());
+        const c10::DeviceGuard device(h0.device());
+        const int64_t T = targets0.numel(), V = w0.size(0), D = w0.size(1);
+        Tensor h, w, targets, lse, rows;
+        const ShapeKey key{{33 | (int64_t)dt << 8, T, V, D, 0, 0, 0, 0}};
+        Need need{};
+        {
+            at::NoGradGuard no_grad;
+            h = h0.contiguous().view({T, D});
+            w = w0.contiguous();
+            targets = targets0.contiguous().view({T});
+            need = need_of(key, [&] {
+                return Need{sigtrain_entropy_workspace_bytes(0, T, V, D, dt, 0), 0, sigtrain_entropy_workspace_bytes(1, T, V, D, dt, 0), 0, 0};
+            });
+            const at::TensorOptions sums = h.options().dtype(dt == ST_F64 ? at::kDouble : at::kFloat);
+            loss = reduction == ST_NONE ? at::empty(targets0.sizes(), sums) : at::empty({}, sums);
+            lse = at::empty({T}, sums);
+            rows = at::empty({1}, sums.dtype(at::kDouble));
+            const Tensor ws = workspace(need.forward, h, [&] { return sigtrain_entropy_workspace_bytes(0, T, V, D, dt, 1); });
+            if (sigtrain_entropy_fwd(h.data_ptr(), w.data_ptr(), targets.data_ptr(), loss.data_ptr(), lse.data_ptr(), rows.data_ptr<double>(), T, V, D,
+                                     reduction, st_index(targets), dt, ws.data_ptr(), (size_t)ws.numel(), current_stream()) != SK_OK)
+                loss.reset();
+        }
+        if (loss.defined() && grad) {
+            auto node = make_node<EntropyNode>();
+            node->set_next_edges(torch::autograd::collect_next_edges(h0, w0));
+            node->h_ = SavedVariable(h, false);
+            node->w_ = SavedVariable(w, false);
+            node->targets_ = SavedVariable(targets, false);
+            node->lse = lse;
+            node->rows = rows;
+            node->reduction = reduction;
+            node->want_h = h0.requires_grad();
+            node->want_w = w0.requires_grad();
+            node->need = need.backward;
+            node->h_sizes = {T, D};
+            node->h_shape = h0.sizes().vec();
+            node->w_sizes = {V, D};
+            node->target_sizes = {T};
+            node->out_sizes = loss.sizes().vec();
+            node->options = h.options();
+            node->out_options = loss.options();
+            node->target_options = targets.options();
+            torch::autograd::set_history(loss, node);
+        }
+    }
+    return wrap(loss);
+}
+
 // The rule for the classes: what a forward call of this shape keeps for its backward call, in bytes (0: nothing), and the flags
 // of that form, forward and backward.
 py::tuple kept_form(bool gram, bool symmetric, int64_t N, int64_t M, int64_t L1, int64_t L2, int64_t d, int lam1, int lam2, int flags,
@@ -551,4 +790,6 @@ PYBIND11_MODULE(_native, m)
     m.def("gram", &gram, py::arg("x"), py::arg("y"), py::arg("lam1"), py::arg("lam2"), py::arg("flags"), py::arg("keep_limit"), all);
     m.def("mmd2", &mmd2);
     m.def("signature", &signature);
+    m.def("embed", &embed);
+    m.def("entropy", &entropy);
 }
