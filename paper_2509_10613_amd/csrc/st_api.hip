@@ -64,6 +64,7 @@ int check_embed(int64_t count, int64_t V, int64_t D, double scale, int it, int d
     if (count < 0 || V < 0 || D < 1 || D > kMostColumns)
         return fail(SK_ERR_SHAPE, "need count >= 0, V >= 0 and 1 <= D <= 2^24 (got %lld, %lld, %lld)", (long long)count, (long long)V, (long long)D);
     if (V > kMostIndex || count > (int64_t)1 << 40) return fail(SK_ERR_SHAPE, "V must stay below 2^31 - 1, count below 2^40");
+    if (count > 0 && D > ((int64_t)1 << 41) / count) return fail(SK_ERR_SHAPE, "more than 2^41 entries");
     if (!std::isfinite(scale)) return fail(SK_ERR_SHAPE, "scale is not finite");
     return SK_OK;
 }

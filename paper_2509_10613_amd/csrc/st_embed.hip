@@ -19,49 +19,69 @@ namespace {
 constexpr int kThreads = 256;
 
 // ------------------------------------------------------------------------------------------------ forward
+// A lane moves U vectors of E entries (16 bytes where a row has as much), all symbols loaded before the first row and all rows before the first
+// store: no branch stands between them.  A row's last vector ends with the row, whatever its length: it may write entries of the one before a second
+// time, with the same values.
+// A: the product's type, double unless the scale is a float (then a float's product, rounded once, is the same number).
 // Index: uint32_t where the number of vectors allows (a 32-bit division per vector instead of a 64-bit one).
-template <typename T, typename Index>
-__global__ __launch_bounds__(kThreads) void embed_fwd_kernel(const void* tokens, int it, const T* table, T* out, int64_t count, int64_t V,
-                                                             int64_t D, sum_t<T> scale, Index per_row, Index items)
+template <typename T, typename A, typename Index, int E, int U>
+__global__ __launch_bounds__(kThreads) void embed_fwd_kernel(const void* tokens, int it, const T* table, T* out, int64_t V, int64_t D, A scale,
+                                                             Index per_row, Index items)
 {
-    constexpr int E = kPer16<T>, U = 4;
-    const Index stride = (Index)gridDim.x * kThreads;
-    for (Index first = (Index)blockIdx.x * kThreads + threadIdx.x; first < items; first += stride * U) {
-        Vec<T, E> v[U];
-        int n[U];
-        T* to[U];
+    const Index first = (Index)blockIdx.x * (kThreads * U) + threadIdx.x;
+    int64_t symbol[U], at[U];
+    int64_t col[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const Index item = first + u * stride;
-            n[u] = 0;
-            if (item >= items || item < first) continue;   // (the second: the sum passed the type's end)
-            const Index row = item / per_row;
-            const int64_t col = (int64_t)(item - row * per_row) * E;
-            const int64_t symbol = load_index(tokens, (int64_t)row, it);
-            n[u] = D - col < E ? (int)(D - col) : E;
-            to[u] = out + (int64_t)row * D + col;
-            const bool there = symbol >= 0 && symbol < V;
-            const T* from = table + (there ? symbol : 0) * D + col;
-            if (!there)
+    for (int u = 0; u < U; ++u) {
+        const Index item = first + u * kThreads < items ? first + u * kThreads : items - 1;
+        const Index row = item / per_row;
+        const int64_t c = (int64_t)(item - row * per_row) * E;
+        col[u] = c <= D - E ? c : D - E;
+        at[u] = (int64_t)row * D + col[u];
+        symbol[u] = load_index(tokens, (int64_t)row, it);
+    }
+    Vec<T, E> v[U];
 #pragma unroll
-                for (int i = 0; i < E; ++i) v[u].v[i] = T(0);
-            else if (n[u] == E) v[u] = load_vec<T, E>(from);
-            else v[u] = load_some<T, E>(from, n[u]);
-        }
+    for (int u = 0; u < U; ++u) v[u] = load_vec<T, E>(table + (symbol[u] >= 0 && symbol[u] < V ? symbol[u] : 0) * D + col[u]);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (n[u] == 0) continue;
+    for (int u = 0; u < U; ++u) {
+        const bool there = symbol[u] >= 0 && symbol[u] < V;
 #pragma unroll
-            for (int i = 0; i < E; ++i) v[u].v[i] = (T)((sum_t<T>)v[u].v[i] * scale);
-            if (n[u] == E) store_vec(to[u], v[u]);
-            else store_some(to[u], v[u], n[u]);
-        }
+        for (int i = 0; i < E; ++i) v[u].v[i] = there ? (T)((A)v[u].v[i] * scale) : T(0);
+        if (first + u * kThreads < items) store_vec(out + at[u], v[u]);
     }
 }
 
+// (a table without rows)
+template <typename T>
+__global__ __launch_bounds__(kThreads) void zeros_kernel(T* out, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) out[i] = T(0);
+}
+
+template <typename T, typename A, int E>
+hipError_t run_fwd(const void* tokens, const T* table, T* out, int64_t count, int64_t V, int64_t D, double scale, int it, hipStream_t st)
+{
+    const int64_t per_row = (D + E - 1) / E, items = count * per_row;
+    const A f = (A)scale;
+    // four vectors per lane; one where that leaves compute units idle.  (Longer batches than a grid holds go in parts.)
+    auto blocks = [&](int64_t vectors) { return (unsigned)((items + vectors - 1) / vectors); };
+    if (items < (int64_t)kThreads * 2048)
+        embed_fwd_kernel<T, A, uint32_t, E, 1><<<blocks(kThreads), kThreads, 0, st>>>(tokens, it, table, out, V, D, f, (uint32_t)per_row, (uint32_t)items);
+    else if (items < (int64_t)1 << 31)
+        embed_fwd_kernel<T, A, uint32_t, E, 4><<<blocks(kThreads * 4), kThreads, 0, st>>>(tokens, it, table, out, V, D, f, (uint32_t)per_row, (uint32_t)items);
+    else
+        embed_fwd_kernel<T, A, uint64_t, E, 4><<<blocks(kThreads * 4), kThreads, 0, st>>>(tokens, it, table, out, V, D, f, (uint64_t)per_row, (uint64_t)items);
+    return hipGetLastError();
+}
+
 // ------------------------------------------------------------------------------------------------ sort
-// A workgroup of 16 waves takes kTile symbols, 512 consecutive ones per wave, in 8 rows of 64.
-constexpr int kSortThreads = 1024, kSortWaves = 16, kSortRows = 8, kTile = kSortThreads * kSortRows, kDigits = 512;
+// A workgroup of 16 waves takes ROWS * 1024 symbols, consecutive ones per wave, in ROWS rows of 64.  Eight rows share the work of counting and
+// scanning among most symbols; two rows give more workgroups while there are few (32768 symbols of 1000, one digit: 4 workgroups and 23 us, or 16).
+constexpr int kSortThreads = 1024, kSortWaves = 16, kManyRows = 8, kFewRows = 2;
+constexpr int kSmall = kSortThreads * kManyRows;   // what one workgroup sorts by itself
+constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;   // at most
+static_assert(kDigits <= kSortThreads);
 
 __device__ __forceinline__ uint32_t symbol_key(const void* tokens, int64_t i, int it, uint32_t V)
 {
@@ -69,14 +89,15 @@ __device__ __forceinline__ uint32_t symbol_key(const void* tokens, int64_t i, in
     return s >= 0 && s < (int64_t)V ? (uint32_t)s : V;   // symbols outside the table go behind all others
 }
 
-// Ranks a wave's 512 symbols by their digit, in order: counts (of the wave, cleared before) ends up with the number of each digit.
-__device__ __forceinline__ void rank_wave(const uint32_t (&key)[kSortRows], const bool (&live)[kSortRows], int shift, int bits,
-                                          volatile uint32_t* counts, uint32_t (&rank)[kSortRows])
+// Ranks a wave's symbols by their digit, in order: counts (of the wave, cleared before) ends up with the number of each digit.
+template <int ROWS>
+__device__ __forceinline__ void rank_wave(const uint32_t (&key)[ROWS], const bool (&live)[ROWS], int shift, int bits, volatile uint32_t* counts,
+                                          uint32_t (&rank)[ROWS])
 {
     const int lane = threadIdx.x & 63;
     const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
-    for (int r = 0; r < kSortRows; ++r) {
+    for (int r = 0; r < ROWS; ++r) {
         const uint32_t digit = key[r] >> shift & ((1u << bits) - 1);
         uint64_t same = __ballot(live[r]);
         for (int b = 0; b < bits; ++b) {
@@ -124,55 +145,58 @@ __device__ __forceinline__ void wave_offsets(uint32_t* counts, uint32_t* scratch
     const int digit = threadIdx.x;
     uint32_t mine = 0;
     if (digit < (1 << bits))
-        for (int w = 0; w < kSortWaves; ++w) mine += counts[w * kDigits + digit];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) mine += counts[(w << bits) + digit];
     uint32_t all;
     const uint32_t local = scan_block(mine, scratch, &all);
     if (digit < (1 << bits)) {
         uint32_t at = begin(digit, local);
+#pragma unroll
         for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = counts[w * kDigits + digit];
-            counts[w * kDigits + digit] = at;
+            const uint32_t c = counts[(w << bits) + digit];
+            counts[(w << bits) + digit] = at;
             at += c;
         }
     }
     __syncthreads();
 }
 
-// Up to kTile symbols: all digits in one launch, symbols and places in registers and LDS.
+// Up to kSmall symbols: all digits in one launch, symbols and places in registers and LDS.
 __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const void* tokens, int it, uint32_t n, uint32_t V, int passes, int bits,
-                                                                  uint32_t* keys, uint32_t* places)
+                                                                  uint32_t* keys, uint32_t* places, uint32_t* list)
 {
+    if (threadIdx.x < 2) list[threadIdx.x] = 0;
     __shared__ uint32_t counts[kSortWaves * kDigits];
-    __shared__ uint32_t key_at[kTile], place_at[kTile];
+    __shared__ uint32_t key_at[kSmall], place_at[kSmall];
     __shared__ uint32_t scratch[kSortWaves];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint32_t key[kSortRows], place[kSortRows], rank[kSortRows];
-    bool live[kSortRows];
+    uint32_t key[kManyRows], place[kManyRows], rank[kManyRows];
+    bool live[kManyRows];
 #pragma unroll
-    for (int r = 0; r < kSortRows; ++r) {
-        const uint32_t i = w * (64 * kSortRows) + r * 64 + lane;
+    for (int r = 0; r < kManyRows; ++r) {
+        const uint32_t i = w * (64 * kManyRows) + r * 64 + lane;
         live[r] = i < n;
         place[r] = i;
         key[r] = live[r] ? symbol_key(tokens, i, it, V) : 0;
     }
     for (int p = 0; p < passes; ++p) {
         const int shift = p * bits;
-        for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortThreads) counts[i] = 0;
+        for (int i = threadIdx.x; i < kSortWaves << bits; i += kSortThreads) counts[i] = 0;
         __syncthreads();
-        rank_wave(key, live, shift, bits, counts + w * kDigits, rank);
+        rank_wave(key, live, shift, bits, counts + (w << bits), rank);
         __syncthreads();
         wave_offsets(counts, scratch, bits, [](int, uint32_t local) { return local; });
 #pragma unroll
-        for (int r = 0; r < kSortRows; ++r)
+        for (int r = 0; r < kManyRows; ++r)
             if (live[r]) {
-                const uint32_t to = counts[w * kDigits + (key[r] >> shift & ((1u << bits) - 1))] + rank[r];
+                const uint32_t to = counts[(w << bits) + (key[r] >> shift & ((1u << bits) - 1))] + rank[r];
                 key_at[to] = key[r];
                 place_at[to] = place[r];
             }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kSortRows; ++r) {
-            const uint32_t i = w * (64 * kSortRows) + r * 64 + lane;
+        for (int r = 0; r < kManyRows; ++r) {
+            const uint32_t i = w * (64 * kManyRows) + r * 64 + lane;
             if (live[r]) {
                 key[r] = key_at[i];
                 place[r] = place_at[i];
@@ -180,8 +204,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const void* to
         }
     }
 #pragma unroll
-    for (int r = 0; r < kSortRows; ++r) {
-        const uint32_t i = w * (64 * kSortRows) + r * 64 + lane;
+    for (int r = 0; r < kManyRows; ++r) {
+        const uint32_t i = w * (64 * kManyRows) + r * 64 + lane;
         if (live[r]) {
             keys[i] = key[r];
             places[i] = place[r];
@@ -189,17 +213,21 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const void* to
     }
 }
 
-// One digit of many symbols, three launches: the digits' numbers in every tile, their running sums (by digit, then by tile),
-// and the symbols to where they go.  keys_in null: the first digit, from the caller's symbols.
+// One digit of many symbols: the digits' numbers in every tile, counts[digit][tile], their running sums (by digit, then by tile), and the symbols to
+// where they go.  Of at most kAddTiles tiles the last launch adds up the numbers itself, counts[tile][digit], which takes it less than a launch in
+// between.  keys_in null: the first digit, from the caller's symbols.
+constexpr int kAddTiles = 128;
+template <int ROWS>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const void* tokens, int it, const uint32_t* keys_in, uint32_t n, uint32_t V,
-                                                                  int shift, int bits, uint32_t* counts)
+                                                                  int shift, int bits, uint32_t* counts, uint32_t* list)
 {
+    if (blockIdx.x == 0 && threadIdx.x < 2) list[threadIdx.x] = 0;
     __shared__ uint32_t bin[kDigits];
     for (int i = threadIdx.x; i < kDigits; i += kSortThreads) bin[i] = 0;
     __syncthreads();
-    const uint64_t base = (uint64_t)blockIdx.x * kTile;
+    const uint64_t base = (uint64_t)blockIdx.x * (ROWS * kSortThreads);
 #pragma unroll
-    for (int r = 0; r < kSortRows; ++r) {
+    for (int r = 0; r < ROWS; ++r) {
         const uint64_t i = base + r * kSortThreads + threadIdx.x;
         if (i < n) {
             const uint32_t key = keys_in ? keys_in[i] : symbol_key(tokens, (int64_t)i, it, V);
@@ -207,32 +235,34 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const void* to
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < (1 << bits); i += kSortThreads) counts[(size_t)i * gridDim.x + blockIdx.x] = bin[i];
+    for (int i = threadIdx.x; i < (1 << bits); i += kSortThreads)
+        counts[gridDim.x <= kAddTiles ? ((size_t)blockIdx.x << bits) + i : (size_t)i * gridDim.x + blockIdx.x] = bin[i];
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_scan_kernel(uint32_t* counts, int64_t entries)
 {
     __shared__ uint32_t scratch[kSortWaves];
+    constexpr int kEach = 8;
     uint32_t before = 0;
-    for (int64_t first = 0; first < entries; first += kSortThreads * 4) {
-        const int64_t i = first + threadIdx.x * 4;
-        uint32_t c[4], sum = 0;
+    for (int64_t first = 0; first < entries; first += kSortThreads * kEach) {
+        const int64_t i = first + threadIdx.x * kEach;
+        uint32_t c[kEach], sum = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            c[j] = i + j < entries ? counts[i + j] : 0;
-            sum += c[j];
-        }
+        for (int j = 0; j < kEach; ++j) c[j] = i + j < entries ? counts[i + j] : 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) sum += c[j];
         uint32_t all;
         uint32_t at = before + scan_block(sum, scratch, &all);
         before += all;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kEach; ++j) {
             if (i + j < entries) counts[i + j] = at;
             at += c[j];
         }
     }
 }
 
+template <int ROWS>
 __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const void* tokens, int it, const uint32_t* keys_in, const uint32_t* places_in,
                                                                  uint32_t n, uint32_t V, int shift, int bits, const uint32_t* begin,
                                                                  uint32_t* keys, uint32_t* places)
@@ -240,24 +270,37 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const void* tok
     __shared__ uint32_t counts[kSortWaves * kDigits];
     __shared__ uint32_t scratch[kSortWaves];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint32_t key[kSortRows], place[kSortRows], rank[kSortRows];
-    bool live[kSortRows];
-    for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortThreads) counts[i] = 0;
+    uint32_t key[ROWS], place[ROWS], rank[ROWS];
+    bool live[ROWS];
+    for (int i = threadIdx.x; i < kSortWaves << bits; i += kSortThreads) counts[i] = 0;
 #pragma unroll
-    for (int r = 0; r < kSortRows; ++r) {
-        const uint64_t i = (uint64_t)blockIdx.x * kTile + w * (64 * kSortRows) + r * 64 + lane;
+    for (int r = 0; r < ROWS; ++r) {
+        const uint64_t i = (uint64_t)blockIdx.x * (ROWS * kSortThreads) + w * (64 * ROWS) + r * 64 + lane;
         live[r] = i < n;
         key[r] = !live[r] ? 0 : keys_in ? keys_in[i] : symbol_key(tokens, (int64_t)i, it, V);
         place[r] = !live[r] ? 0 : keys_in ? places_in[i] : (uint32_t)i;
     }
     __syncthreads();
-    rank_wave(key, live, shift, bits, counts + w * kDigits, rank);
+    rank_wave(key, live, shift, bits, counts + (w << bits), rank);
     __syncthreads();
-    wave_offsets(counts, scratch, bits, [&](int digit, uint32_t) { return begin[(size_t)digit * gridDim.x + blockIdx.x]; });
+    if (gridDim.x <= kAddTiles) {
+        uint32_t before = 0, total = 0, all;
+        if (threadIdx.x < 1 << bits)
+#pragma unroll 8
+            for (uint32_t t = 0; t < gridDim.x; ++t) {
+                const uint32_t c = begin[((size_t)t << bits) + threadIdx.x];
+                total += c;
+                before += t < blockIdx.x ? c : 0;
+            }
+        before += scan_block(total, scratch, &all);
+        wave_offsets(counts, scratch, bits, [&](int, uint32_t) { return before; });
+    } else {
+        wave_offsets(counts, scratch, bits, [&](int digit, uint32_t) { return begin[(size_t)digit * gridDim.x + blockIdx.x]; });
+    }
 #pragma unroll
-    for (int r = 0; r < kSortRows; ++r)
+    for (int r = 0; r < ROWS; ++r)
         if (live[r]) {
-            const uint32_t to = counts[w * kDigits + (key[r] >> shift & ((1u << bits) - 1))] + rank[r];
+            const uint32_t to = counts[(w << bits) + (key[r] >> shift & ((1u << bits) - 1))] + rank[r];
             keys[to] = key[r];
             places[to] = place[r];
         }
@@ -286,12 +329,18 @@ __device__ __forceinline__ uint32_t symbols_before(const uint32_t* keys, int64_t
     return (uint32_t)lo;
 }
 
-// What a unit hands over (rows: -1 for nothing): the sum of the row it has not finished, and the last part of the row it finished but
-// did not begin.
+// What a unit hands over: the sum of the row it has not finished, and the last part of the row it finished but did not begin.  The units of the
+// latter kind are listed with their rows and the symbols before them (in the order they come; what is made of one does not depend on the others),
+// those whose row has symbols kLong units before in a list of their own.
+constexpr int kLong = 8;
+struct Listed {
+    uint32_t unit, row, before;
+};
 template <typename A>
 struct Handed {
-    A *carry, *head;                 // [units][D]
-    int64_t *carry_row, *head_row;   // [units]
+    A *carry, *head;       // [units][D]
+    uint32_t* many;        // entries of both lists, cleared by the sort's first launch
+    Listed* list[2];       // short, long
 };
 
 template <typename T>
@@ -345,6 +394,10 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const T* grad, T* 
     const int width = D - col >= E ? E : D > col ? (int)(D - col) : 0;
     bool wrote = false, some = false;
     const int64_t first_row = row;
+    Vec<T, E> zeros;
+#pragma unroll
+    for (int i = 0; i < E; ++i) zeros.v[i] = T(0);
+    T* to = out + row * D + col;
     A sum[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) sum[i] = 0;
@@ -375,15 +428,20 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const T* grad, T* 
 #pragma unroll
                     for (int i = 0; i < E; ++i)
                         if (i < width) handed.head[at * D + col + i] = sum[i];
+            } else if (!some) {   // (a symbol that does not occur)
+                if (width == E) store_vec(to, zeros);
+                else if (width > 0) store_some(to, zeros, width);
             } else if (width > 0) {
                 Vec<T, E> r;
 #pragma unroll
                 for (int i = 0; i < E; ++i) r.v[i] = (T)(sum[i] * scale);
-                if (width == E) store_vec(out + row * D + col, r);
-                else store_some(out + row * D + col, r, width);
+                if (width == E) store_vec(to, r);
+                else store_some(to, r, width);
             }
+            if (some || begun)
 #pragma unroll
-            for (int i = 0; i < E; ++i) sum[i] = 0;
+                for (int i = 0; i < E; ++i) sum[i] = 0;
+            to += D;
             wrote = true;
             some = false;
             ++row;
@@ -394,42 +452,82 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const T* grad, T* 
 #pragma unroll
         for (int i = 0; i < E; ++i)
             if (i < width) handed.carry[at * D + col + i] = sum[i];
-    if (lane == 0 && blockIdx.y == 0) {
-        handed.carry_row[at] = carries ? row : -1;
-        handed.head_row[at] = begun && wrote ? first_row : -1;
+    if (lane == 0 && blockIdx.y == 0 && begun && wrote) {
+        const int64_t back = before - 1 - (int64_t)kLong * events;
+        const bool is_long = back >= 0 && keys[back] == (uint32_t)first_row;
+        // (one atomic addition for all units of the wave)
+        const uint64_t longs = __ballot(is_long), shorts = __ballot(!is_long), mine = is_long ? longs : shorts;
+        const int self = threadIdx.x & 63, leader = __ffsll((unsigned long long)mine) - 1;
+        uint32_t place = 0;
+        if (self == leader) place = atomicAdd(handed.many + is_long, (uint32_t)__popcll(mine));
+        place = __shfl(place, leader) + __popcll(mine & (((uint64_t)1 << self) - 1));
+        handed.list[is_long][place] = {(uint32_t)at, (uint32_t)first_row, (uint32_t)before};
     }
 }
 
-// Rows that more than one unit added to: the units' sums in their order.
+// Rows that more than one unit added to: the units' sums in their order, from the one with the row's first symbol on.  Of a frequent symbol's row (of
+// thousands of units, it may be) a workgroup takes 64 columns, each wave a quarter of the units; of the others a workgroup takes kShare columns.
+constexpr int kJoinWaves = 4, kShare = 512;
+template <typename A>
+__device__ __forceinline__ A carried(const A* carry, int64_t from, int64_t to, int64_t D, int64_t c)
+{
+    A sum = 0;
+    int64_t i = from;
+    for (; i + 8 <= to; i += 8) {
+        A part[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part[j] = carry[(i + j) * D + c];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += part[j];
+    }
+    for (; i < to; ++i) sum += carry[i * D + c];
+    return sum;
+}
 template <typename T>
-__global__ __launch_bounds__(kThreads) void embed_join_kernel(T* out, int64_t D, sum_t<T> scale, Handed<sum_t<T>> handed)
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(T* out, const uint32_t* keys, int64_t D, int events, sum_t<T> scale,
+                                                                     Handed<sum_t<T>> handed)
 {
     using A = sum_t<T>;
-    const int64_t u = blockIdx.x, row = handed.head_row[u];
-    if (row < 0) return;
-    const int lane = threadIdx.x & 63;
-    int64_t first = u;   // the first unit that carries this row
-    for (;;) {
-        const int64_t at = first - 1 - lane;
-        const uint64_t other = __ballot(at < 0 || handed.carry_row[at < 0 ? 0 : at] != row);
-        if (other) {
-            first -= __ffsll((unsigned long long)other) - 1;
-            break;
+    __shared__ A parts[kJoinWaves][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint32_t slices = (uint32_t)((D + 63) / 64);
+    const uint32_t shares = (uint32_t)((D + kShare - 1) / kShare);
+    const uint64_t few = (uint64_t)handed.many[0] * shares, many = (uint64_t)handed.many[1] * slices;
+    for (uint64_t task = blockIdx.x; task < few + many; task += gridDim.x) {
+        const bool is_long = task < many;
+        const Listed l = is_long ? handed.list[1][task / slices] : handed.list[0][(task - many) / shares];
+        // the row's first symbol
+        int64_t lo = is_long ? 0 : (int64_t)l.before - 1 - (int64_t)kLong * events, hi = (int64_t)l.before - 1;
+        if (lo < 0) lo = 0;
+        while (lo < hi) {
+            const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+            const bool in = at < hi;
+            const uint64_t probes = __ballot(in), yes = __ballot(in && keys[in ? at : lo] >= l.row);
+            if (yes == 0) {
+                lo += (63 - __clzll(probes)) * step + 1;
+            } else {
+                const int f = __ffsll((unsigned long long)yes) - 1;
+                hi = lo + f * step;
+                if (f > 0) lo = hi - step + 1;
+            }
         }
-        first -= 64;
-    }
-    for (int64_t c = (int64_t)blockIdx.y * kThreads + threadIdx.x; c < D; c += (int64_t)gridDim.y * kThreads) {
-        A sum = 0;
-        int64_t i = first;
-        for (; i + 8 <= u; i += 8) {
-            A part[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) part[j] = handed.carry[(i + j) * D + c];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum += part[j];
+        const int64_t u = l.unit, row = l.row, first = (lo + row) / events;
+        if (!is_long) {
+            const int64_t c0 = (int64_t)((task - many) % shares) * kShare, c1 = c0 + kShare < D ? c0 + kShare : D;
+            for (int64_t c = c0 + threadIdx.x; c < c1; c += 64 * kJoinWaves)
+                out[row * D + c] = (T)((carried(handed.carry, first, u, D, c) + handed.head[u * D + c]) * scale);
+            continue;
         }
-        for (; i < u; ++i) sum += handed.carry[i * D + c];
-        out[row * D + c] = (T)((sum + handed.head[u * D + c]) * scale);
+        const int64_t c = (int64_t)(task % slices) * 64 + lane;
+        parts[w][lane] = c < D ? carried(handed.carry, first + (u - first) * w / kJoinWaves, first + (u - first) * (w + 1) / kJoinWaves, D, c) : (A)0;
+        __syncthreads();
+        if (w == 0 && c < D) {
+            A all = 0;
+#pragma unroll
+            for (int j = 0; j < kJoinWaves; ++j) all += parts[j][lane];
+            out[row * D + c] = (T)((all + handed.head[u * D + c]) * scale);
+        }
+        __syncthreads();
     }
 }
 
@@ -451,20 +549,25 @@ hipError_t embed_fwd(const void* tokens, const void* table, void* out, int64_t c
 {
     return by_type(dt, [&](auto type) {
         using T = decltype(type);
-        const int64_t per_row = (D + kPer16<T> - 1) / kPer16<T>, items = count * per_row;
-        int64_t blocks = (items + kThreads * 4 - 1) / (kThreads * 4);
-        // few vectors: one per lane, on as many compute units as there are
-        if (blocks < 1024) blocks = (items + kThreads - 1) / kThreads < 1024 ? (items + kThreads - 1) / kThreads : 1024;
-        if (blocks > 65536) blocks = 65536;
         const T* from = static_cast<const T*>(table);
         T* to = static_cast<T*>(out);
-        if (items < (int64_t)1 << 31)
-            embed_fwd_kernel<T, uint32_t><<<(unsigned)blocks, kThreads, 0, st>>>(tokens, it, from, to, count, V, D, (sum_t<T>)scale,
-                                                                                   (uint32_t)per_row, (uint32_t)items);
-        else
-            embed_fwd_kernel<T, uint64_t><<<(unsigned)blocks, kThreads, 0, st>>>(tokens, it, from, to, count, V, D, (sum_t<T>)scale,
-                                                                                   (uint64_t)per_row, (uint64_t)items);
-        return hipGetLastError();
+        if (V == 0) {
+            const int64_t blocks = (count * D + kThreads - 1) / kThreads;
+            zeros_kernel<T><<<(unsigned)(blocks < 16384 ? blocks : 16384), kThreads, 0, st>>>(to, count * D);
+            return hipGetLastError();
+        }
+        auto by_width = [&](auto a) {
+            using A = decltype(a);
+            if (D >= kPer16<T>) return run_fwd<T, A, kPer16<T>>(tokens, from, to, count, V, D, scale, it, st);
+            if constexpr (kPer16<T> > 4)
+                if (D >= 4) return run_fwd<T, A, 4>(tokens, from, to, count, V, D, scale, it, st);
+            if constexpr (kPer16<T> > 2)
+                if (D >= 2) return run_fwd<T, A, 2>(tokens, from, to, count, V, D, scale, it, st);
+            return run_fwd<T, A, 1>(tokens, from, to, count, V, D, scale, it, st);
+        };
+        if constexpr (sizeof(T) == 4)
+            if ((double)(float)scale == scale) return by_width(float{});
+        return by_width(sum_t<T>{});
     });
 }
 
@@ -479,15 +582,19 @@ EmbedPlan embed_plan(int64_t count, int64_t V, int64_t D, int dt)
     p.lanes = 1;
     while (p.lanes < vectors && p.lanes < kThreads) p.lanes *= 2;
     p.slices = (int)((vectors + p.lanes - 1) / p.lanes);
-    p.events = 32;
-    p.units = (count + V + p.events - 1) / p.events;
     const int per_group = kThreads / p.lanes;
+    // 32 events share the search for their beginning; fewer while there are not two workgroups for every compute unit
+    p.events = 32;
+    while (p.events > 8 && (count + V) / (p.events * per_group) * p.slices < 512) p.events /= 2;
+    p.units = (count + V + p.events - 1) / p.events;
     p.groups = (p.units + per_group - 1) / per_group;
     int bits = 1;
     while (bits < 32 && ((uint64_t)V >> bits) != 0) ++bits;   // the largest key is V
-    p.passes = (bits + 8) / 9;
+    p.passes = (bits + kDigitBits - 1) / kDigitBits;
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.tiles = count <= kTile ? 0 : (count + kTile - 1) / kTile;
+    p.rows = count <= 128 * kSortThreads ? kFewRows : kManyRows;
+    const int64_t tile = (int64_t)p.rows * kSortThreads;
+    p.tiles = count <= kSmall ? 0 : (count + tile - 1) / tile;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -503,7 +610,7 @@ EmbedPlan embed_plan(int64_t count, int64_t V, int64_t D, int dt)
     const int64_t slots = p.groups * per_group;
     p.off_carry = take((size_t)slots * D * sum_size);
     p.off_head = take((size_t)slots * D * sum_size);
-    p.off_rows = take((size_t)slots * 16);
+    p.off_list = take(256 + (size_t)p.units * 2 * sizeof(Listed));
     p.total = at;
     return p;
 }
@@ -514,24 +621,28 @@ hipError_t embed_bwd(const EmbedPlan& p, const void* tokens, const void* grad_ou
     unsigned char* base = static_cast<unsigned char*>(ws);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(base + p.off_keys[0]), reinterpret_cast<uint32_t*>(base + p.off_keys[1])};
     uint32_t* places[2] = {reinterpret_cast<uint32_t*>(base + p.off_places[0]), reinterpret_cast<uint32_t*>(base + p.off_places[1])};
+    uint32_t* list = reinterpret_cast<uint32_t*>(base + p.off_list);
     const uint32_t n = (uint32_t)p.count, V = (uint32_t)p.V;
     hipError_t e;
     int from = 0;
     if (n == 0) {
     } else if (p.tiles == 0) {
-        sort_small_kernel<<<1, kSortThreads, 0, st>>>(tokens, it, n, V, p.passes, p.bits, keys[0], places[0]);
+        sort_small_kernel<<<1, kSortThreads, 0, st>>>(tokens, it, n, V, p.passes, p.bits, keys[0], places[0], list);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     } else {
         uint32_t* counts = reinterpret_cast<uint32_t*>(base + p.off_counts);
         for (int i = 0; i < p.passes; ++i) {
             const uint32_t *keys_in = i ? keys[from] : nullptr, *places_in = i ? places[from] : nullptr;
             const int to = i ? 1 - from : 0, shift = i * p.bits;
-            sort_count_kernel<<<(unsigned)p.tiles, kSortThreads, 0, st>>>(tokens, it, keys_in, n, V, shift, p.bits, counts);
+            const auto count = p.rows == kFewRows ? sort_count_kernel<kFewRows> : sort_count_kernel<kManyRows>;
+            count<<<(unsigned)p.tiles, kSortThreads, 0, st>>>(tokens, it, keys_in, n, V, shift, p.bits, counts, list);
             if ((e = hipGetLastError()) != hipSuccess) return e;
-            sort_scan_kernel<<<1, kSortThreads, 0, st>>>(counts, p.tiles << p.bits);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-            sort_move_kernel<<<(unsigned)p.tiles, kSortThreads, 0, st>>>(tokens, it, keys_in, places_in, n, V, shift, p.bits, counts, keys[to],
-                                                                         places[to]);
+            if (p.tiles > kAddTiles) {
+                sort_scan_kernel<<<1, kSortThreads, 0, st>>>(counts, p.tiles << p.bits);
+                if ((e = hipGetLastError()) != hipSuccess) return e;
+            }
+            const auto move = p.rows == kFewRows ? sort_move_kernel<kFewRows> : sort_move_kernel<kManyRows>;
+            move<<<(unsigned)p.tiles, kSortThreads, 0, st>>>(tokens, it, keys_in, places_in, n, V, shift, p.bits, counts, keys[to], places[to]);
             if ((e = hipGetLastError()) != hipSuccess) return e;
             from = to;
         }
@@ -539,18 +650,18 @@ hipError_t embed_bwd(const EmbedPlan& p, const void* tokens, const void* grad_ou
     return by_type(dt, [&](auto type) {
         using T = decltype(type);
         using A = sum_t<T>;
-        const int64_t slots = p.groups * (kThreads / p.lanes);
-        int64_t* rows = reinterpret_cast<int64_t*>(base + p.off_rows);
-        const Handed<A> handed{reinterpret_cast<A*>(base + p.off_carry), reinterpret_cast<A*>(base + p.off_head), rows, rows + slots};
+        const Handed<A> handed{reinterpret_cast<A*>(base + p.off_carry), reinterpret_cast<A*>(base + p.off_head), list,
+                               {reinterpret_cast<Listed*>(list + 64), reinterpret_cast<Listed*>(list + 64) + p.units}};
         const size_t lds = (size_t)(kThreads / p.lanes) * p.events * 4;
         embed_sums_kernel<T><<<dim3((unsigned)p.groups, p.slices), kThreads, lds, st>>>(
             static_cast<const T*>(grad_out), static_cast<T*>(grad_table), keys[from], places[from], p.count, p.V, p.D, p.lanes, p.events,
             (A)scale, handed);
         hipError_t err = hipGetLastError();
         if (err != hipSuccess || p.count == 0) return err;
-        const int64_t slices = (p.D + kThreads - 1) / kThreads;
-        embed_join_kernel<T><<<dim3((unsigned)p.units, (unsigned)(slices < 16 ? slices : 16)), kThreads, 0, st>>>(static_cast<T*>(grad_table), p.D,
-                                                                                                                (A)scale, handed);
+        // (as many workgroups as run at once take the list in turns)
+        const int64_t most = p.units * 2;
+        embed_join_kernel<T><<<(unsigned)(most < 2048 ? most : 2048), 64 * kJoinWaves, 0, st>>>(static_cast<T*>(grad_table), keys[from], p.D, p.events, (A)scale,
+                                                                                             handed);
         return hipGetLastError();
     });
 }

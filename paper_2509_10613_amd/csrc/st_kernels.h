@@ -24,8 +24,9 @@ struct EmbedPlan {
     int events;           // tokens added and rows written per unit
     int64_t units, groups;   // units; workgroups of them
     int passes, bits;     // of the sort: digits, bits per digit
+    int rows;             // ... rows of 64 symbols per wave
     int64_t tiles;        // ... and workgroups (0: one workgroup sorts everything)
-    size_t off_keys[2], off_places[2], off_counts, off_carry, off_head, off_rows, total;
+    size_t off_keys[2], off_places[2], off_counts, off_carry, off_head, off_list, total;
 };
 EmbedPlan embed_plan(int64_t count, int64_t V, int64_t D, int dt);
 hipError_t embed_bwd(const EmbedPlan& p, const void* tokens, const void* grad_out, void* grad_table, double scale, int it, int dt, void* ws,

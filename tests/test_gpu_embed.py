@@ -200,3 +200,10 @@ def test_another_stream_and_a_captured_graph():
 def test_gradient_against_differences():
     tokens, table, _ = make(6, (5, 4), 6, 3, torch.float64)
     assert torch.autograd.gradcheck(lambda t: ska.embed(tokens.cuda(), t, 1.3), (table.cuda().requires_grad_(),))
+
+
+def test_more_tokens_than_the_last_launch_of_a_digit_adds_up():
+    """More than 128 tiles of 8192 symbols: three launches per digit."""
+    for V in (700, 40000):
+        tokens, table, up = make(V, (1100000,), V, 3, torch.float32, skew=True)
+        check(tokens, table, up, 1.5, *both(tokens, table, up, 1.5))
