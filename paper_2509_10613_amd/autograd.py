@@ -291,7 +291,8 @@ def grad_norm(grads):
     """The Euclidean norm of all entries of a tensor or of several (of any floating types and layouts, on one device), as a float64 [] on
     the device."""
     grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
-    return sk.grad_norm([g.detach().contiguous() for g in grads])
+    norm = _native.clip(grads, None, 0.0)
+    return sk.grad_norm([g.detach().contiguous() for g in grads]) if norm is None else norm
 
 
 def clip_grad_norm(grads, max_norm, out=None):
@@ -301,6 +302,9 @@ def clip_grad_norm(grads, max_norm, out=None):
     other layouts than contiguous ones go through copies."""
     grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
     outs = grads if out is None else ([out] if isinstance(out, torch.Tensor) else list(out))
+    norm = _native.clip(grads, outs, float(max_norm))
+    if norm is not None:
+        return norm
     with torch.no_grad():
         dense = [g.contiguous() for g in grads]
         if out is None:

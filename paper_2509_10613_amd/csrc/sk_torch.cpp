@@ -769,6 +769,64 @@ py::object entropy(py::object ho, py::object wo, py::object to, const std::strin
     return wrap(loss);
 }
 
+// Plain contiguous device tensors of one device, with their addresses and types.
+struct Arrays {
+    std::vector<Tensor> tensors;
+    std::vector<void*> at;
+    std::vector<int64_t> counts;
+    std::vector<int> dts;
+};
+bool arrays(const py::list& list, Arrays& a)
+{
+    const size_t n = list.size();
+    a.tensors.resize(n);
+    a.at.resize(n);
+    a.counts.resize(n);
+    a.dts.resize(n);
+    for (size_t i = 0; i < n; ++i) {
+        Tensor& t = a.tensors[i];
+        st_dtype dt;
+        if (!plain_st(list[i], t, dt) || !t.is_contiguous() || t.device() != a.tensors[0].device()) return false;
+        a.at[i] = t.numel() > 0 ? t.data_ptr() : nullptr;
+        a.counts[i] = t.numel();
+        a.dts[i] = dt;
+    }
+    return true;
+}
+
+// outs None: the norm alone; the list itself: in place
+py::object clip(py::list grads, py::object outs, double max_norm)
+{
+    Arrays g, o;
+    const bool scale = !outs.is_none(), in_place = scale && outs.ptr() == grads.ptr();
+    if (transformed() || grads.size() == 0 || !arrays(grads, g)) return py::none();
+    if (scale && !in_place) {
+        const py::list list = py::reinterpret_borrow<py::list>(outs);
+        if (list.size() != grads.size() || !arrays(list, o) || o.tensors[0].device() != g.tensors[0].device()) return py::none();
+        for (size_t i = 0; i < o.tensors.size(); ++i)
+            if (o.tensors[i].sizes() != g.tensors[i].sizes()) return py::none();
+    }
+    Tensor norm;
+    {
+        py::gil_scoped_release release;
+        at::NoGradGuard no_grad;
+        const c10::DeviceGuard device(g.tensors[0].device());
+        const int64_t n = (int64_t)g.tensors.size();
+        norm = at::empty({}, g.tensors[0].options().dtype(at::kDouble));
+        const Tensor ws = bytes(sigtrain_clip_workspace_bytes(n), norm);
+        const Arrays& to = in_place ? g : o;
+        const int rc = scale ? sigtrain_clip(g.at.data(), to.at.data(), g.counts.data(), g.dts.data(), to.dts.data(), n, max_norm, norm.data_ptr<double>(),
+                                             ws.data_ptr(), (size_t)ws.numel(), current_stream())
+                             : sigtrain_grad_norm(g.at.data(), g.counts.data(), g.dts.data(), n, norm.data_ptr<double>(), ws.data_ptr(),
+                                                  (size_t)ws.numel(), current_stream());
+        if (rc != SK_OK) norm.reset();
+        else if (scale)
+            for (const Tensor& t : to.tensors)
+                if (!t.is_inference()) torch::autograd::impl::bump_version(t);
+    }
+    return wrap(norm);
+}
+
 // The rule for the classes: what a forward call of this shape keeps for its backward call, in bytes (0: nothing), and the flags
 // of that form, forward and backward.
 py::tuple kept_form(bool gram, bool symmetric, int64_t N, int64_t M, int64_t L1, int64_t L2, int64_t d, int lam1, int lam2, int flags,
@@ -792,4 +850,5 @@ PYBIND11_MODULE(_native, m)
     m.def("signature", &signature);
     m.def("embed", &embed);
     m.def("entropy", &entropy);
+    m.def("clip", &clip);
 }
