@@ -444,6 +444,13 @@ def _scratch(nbytes, device, least=None):
             size = max(size // 2, few)
 
 
+def _given(ws, device):
+    """A caller's scratch: bytes on the call's device."""
+    if ws.dtype != torch.uint8 or ws.device != device:
+        raise ValueError("ws must be uint8 on %s, got %s on %s" % (device, ws.dtype, ws.device))
+    return _dev(ws, "ws")
+
+
 def embed_fwd(tokens, table, scale=1.0, out=None):
     """out[..., :] = scale * table[tokens[...], :] for tokens of any shape and table[V, D]; zeros where a token is outside 0 .. V - 1."""
     _dev(tokens, "tokens"); _dev(table, "table")
@@ -464,7 +471,7 @@ def embed_fwd(tokens, table, scale=1.0, out=None):
 def embed_bwd(tokens, grad_out, V, scale=1.0, grad_table=None, ws=None):
     """dF/dtable [V, D] for upstream gradients grad_out[..., D]: the rows of every symbol summed in a fixed order."""
     _dev(tokens, "tokens"); _dev(grad_out, "grad_out")
-    _together(grad_out, tokens, grad_table, ws)
+    _together(grad_out, tokens, grad_table)
     D = grad_out.shape[-1] if grad_out.dim() else 0
     if tuple(grad_out.shape) != (*tokens.shape, D):
         raise ValueError("grad_out must be [*tokens.shape, D], got %s and %s" % (tuple(tokens.shape), tuple(grad_out.shape)))
@@ -477,6 +484,7 @@ def embed_bwd(tokens, grad_out, V, scale=1.0, grad_table=None, ws=None):
     with torch.cuda.device(grad_out.device):
         if ws is None:
             ws = _scratch(load().sigtrain_embed_bwd_workspace_bytes(n, V, D, dt), grad_out.device)
+        _given(ws, grad_out.device)
         _check(load().sigtrain_embed_bwd(_ptr(tokens), _ptr(grad_out), _ptr(grad_table), n, V, D, scale, it, dt, _ptr(ws), ws.numel(),
                                          _stream()))
     return grad_table
@@ -506,6 +514,7 @@ def entropy_fwd(h, w, targets, reduction="mean", ws=None):
     with torch.cuda.device(h.device):
         if ws is None:
             ws = _scratch(size(0, T, V, D, dt, 0), h.device, lambda: size(0, T, V, D, dt, 1))
+        _given(ws, h.device)
         _check(load().sigtrain_entropy_fwd(_ptr(h), _ptr(w), _ptr(targets), _ptr(loss), _ptr(lse), _ptr(rows), T, V, D, red, it, dt, _ptr(ws),
                                            ws.numel(), _stream()))
     return loss, lse, rows
@@ -526,6 +535,7 @@ def entropy_bwd(h, w, targets, lse, rows, grad, reduction="mean", want_h=True, w
     with torch.cuda.device(h.device):
         if ws is None:
             ws = _scratch(size(1, T, V, D, dt, 0), h.device, lambda: size(1, T, V, D, dt, 1))
+        _given(ws, h.device)
         _check(load().sigtrain_entropy_bwd(_ptr(h), _ptr(w), _ptr(targets), _ptr(lse), _ptr(rows), _ptr(grad), _ptr(gh), _ptr(gw), T, V, D, red,
                                            it, dt, _ptr(ws), ws.numel(), _stream()))
     return gh, gw

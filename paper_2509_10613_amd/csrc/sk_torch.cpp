@@ -377,7 +377,7 @@ struct EntropyNode : public Node {
     int reduction = ST_MEAN;
     bool want_h = false, want_w = false;
     size_t need = 0;
-    std::vector<int64_t> h_sizes, h_shape, w_sizes, target_sizes, out_sizes;   // h_shape: as the caller's
+    std::vector<int64_t> h_sizes, w_sizes, target_sizes, out_sizes;
     at::TensorOptions options, out_options, target_options;
     std::string name() const override { return "LinearCrossEntropyBackward"; }
     void release_variables() override
@@ -412,8 +412,8 @@ struct EntropyNode : public Node {
             expect(g, "the upstream gradient", out_sizes, out_options);
             st_dtype dt = ST_F32;
             st_type(h, dt);
-            const int64_t T = h_sizes[0], D = h_sizes[1], V = w_sizes[0];
-            if (want_h) out[0] = at::empty(h_shape, options);
+            const int64_t T = targets.numel(), V = w_sizes[0], D = w_sizes[1];
+            if (want_h) out[0] = at::empty(h_sizes, options);
             if (want_w) out[1] = at::empty(w_sizes, options);
             const Tensor ws = workspace(need, h, [&] { return sigtrain_entropy_workspace_bytes(1, T, V, D, dt, 1); });
             check(sigtrain_entropy_bwd(h.data_ptr(), w.data_ptr(), targets.data_ptr(), l.data_ptr(), n.data_ptr<double>(), g.data_ptr(), ptr(out[0]),
@@ -728,9 +728,9 @@ py::object entropy(py::object ho, py::object wo, py::object to, const std::strin
         Need need{};
         {
             at::NoGradGuard no_grad;
-            h = h0.contiguous().view({T, D});
+            h = h0.contiguous();
             w = w0.contiguous();
-            targets = targets0.contiguous().view({T});
+            targets = targets0.contiguous();
             need = need_of(key, [&] {
                 return Need{sigtrain_entropy_workspace_bytes(0, T, V, D, dt, 0), 0, sigtrain_entropy_workspace_bytes(1, T, V, D, dt, 0), 0, 0};
             });
@@ -755,10 +755,9 @@ py::object entropy(py::object ho, py::object wo, py::object to, const std::strin
             node->want_h = h0.requires_grad();
             node->want_w = w0.requires_grad();
             node->need = need.backward;
-            node->h_sizes = {T, D};
-            node->h_shape = h0.sizes().vec();
+            node->h_sizes = h.sizes().vec();
             node->w_sizes = {V, D};
-            node->target_sizes = {T};
+            node->target_sizes = targets.sizes().vec();
             node->out_sizes = loss.sizes().vec();
             node->options = h.options();
             node->out_options = loss.options();

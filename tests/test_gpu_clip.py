@@ -158,3 +158,23 @@ def test_in_place_scaling_is_seen_by_autograd():
     ska.clip_grad_norm(x, 1e-3)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+def test_refusals():
+    a, b = torch.randn(8, device="cuda"), torch.randn(4, device="cuda")
+    with pytest.raises(sk.SigKernelError, match="overlaps"):
+        ska.clip_grad_norm([a, a], 1.0)
+    with pytest.raises(sk.SigKernelError, match="overlaps"):
+        ska.clip_grad_norm([a[:6], a[4:]], 1.0)
+    with pytest.raises(sk.SigKernelError, match="negative or NaN"):
+        ska.clip_grad_norm([a], -1.0)
+    with pytest.raises(ValueError, match="outputs"):
+        ska.clip_grad_norm([a, b], 1.0, out=[a])
+    with pytest.raises(ValueError, match="shape"):
+        ska.clip_grad_norm([a], 1.0, out=[b])
+    with pytest.raises(TypeError):
+        ska.grad_norm([a.int()])
+    before = a.clone()
+    with pytest.raises(TypeError):
+        ska.clip_grad_norm([a, b.long()], 1e-3)
+    assert torch.equal(a, before)

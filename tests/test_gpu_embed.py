@@ -207,3 +207,35 @@ def test_more_tokens_than_the_last_launch_of_a_digit_adds_up():
     for V in (700, 40000):
         tokens, table, up = make(V, (1100000,), V, 3, torch.float32, skew=True)
         check(tokens, table, up, 1.5, *both(tokens, table, up, 1.5))
+
+
+def test_what_lies_behind_a_workspace_stays():
+    for dtype in TYPES:
+        for n, V, D in ((100, 30, 7), (9000, 50, 5), (300, 4, 600)):
+            tokens, table, up = make(n, (n,), V, D, dtype, skew=True)
+            size = int(sk.load().sigtrain_embed_bwd_workspace_bytes(n, V, D, sk._ST_TYPES[dtype]))
+            ws = torch.full((size + 4096,), 77, dtype=torch.uint8, device="cuda")
+            out = torch.full((V * D + 64,), 7.0, dtype=dtype, device="cuda")
+            sk.embed_bwd(tokens.cuda(), up.cuda(), V, 1.0, grad_table=out[:V * D].view(V, D), ws=ws[:size])
+            assert torch.all(ws[size:] == 77) and torch.all(out[V * D:] == 7.0)
+            rows = torch.full((n * D + 64,), 7.0, dtype=dtype, device="cuda")
+            sk.embed_fwd(tokens.cuda(), table.cuda(), 1.0, out=rows[:n * D].view(n, D))
+            assert torch.all(rows[n * D:] == 7.0)
+
+
+def test_a_table_without_rows():
+    out = sk.embed_fwd(torch.arange(5, device="cuda"), torch.empty((0, 3), device="cuda"))
+    assert out.shape == (5, 3) and torch.all(out == 0)
+
+
+def test_restored_tokens_and_shapes():
+    tokens, table, up = make(31, (4, 6), 9, 5, torch.float64)
+    want = both(tokens, table, up, 1.0)
+    t = table.cuda().requires_grad_()
+    with torch.autograd.graph.save_on_cpu():
+        out = ska.embed(tokens.cuda(), t)
+    (grad,) = torch.autograd.grad(out, [t], up.cuda())
+    assert torch.equal(out.detach(), want[0]) and torch.equal(grad, want[1])
+    out = ska.embed(tokens[0, 0].cuda(), t)
+    assert out.shape == (5,)
+    assert ska.embed(tokens[:0].cuda(), t).shape == (0, 6, 5)

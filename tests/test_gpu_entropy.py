@@ -245,3 +245,122 @@ def test_many_classes():
     T, V, D = 64, 200001, 1024
     h, w, targets = make(14, T, V, D, torch.bfloat16, outside=0.0)
     check(h, w, targets, "mean", *run(h, w, targets))
+
+
+# several pieces of few rows, of logits in parts (few tiles of many steps), of rows in steps of their own; between the least workspace and the best
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V,D", [(9, 1300, 50), (16, 700, 128), (40, 900, 9000), (300, 1100, 136)])
+def test_pieces_of_other_shapes(T, V, D, dtype):
+    h, w, targets = make(T + D, T, V, D, dtype)
+    hd, wd, td = h.cuda(), w.cuda(), targets.cuda()
+    dt = sk._ST_TYPES[dtype]
+    size = sk.load().sigtrain_entropy_workspace_bytes
+    for part in (0.0, 0.5, 1.0):
+        sizes = [int(size(b, T, V, D, dt, 1) + part * (size(b, T, V, D, dt, 0) - size(b, T, V, D, dt, 1))) for b in (0, 1)]
+        ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+        loss, lse, rows = sk.entropy_fwd(hd, wd, td, "sum", ws=ws[0])
+        up = torch.tensor(-1.3, dtype=loss.dtype)
+        gh, gw = sk.entropy_bwd(hd, wd, td, lse, rows, up.cuda(), "sum", ws=ws[1])
+        check(h, w, targets, "sum", up, loss, gh, gw)
+
+
+def test_what_lies_behind_a_workspace_stays():
+    """Nothing is written past the bytes that were given, nor past the last row of an output."""
+    for dtype in TYPES:
+        for T, V, D in ((7, 300, 33), (130, 500, 64), (40, 300, 9000)):
+            h, w, targets = make(T, T, V, D, dtype)
+            hd, wd, td = h.cuda(), w.cuda(), targets.cuda()
+            size = sk.load().sigtrain_entropy_workspace_bytes
+            for least in (0, 1):
+                sizes = [int(size(b, T, V, D, sk._ST_TYPES[dtype], least)) for b in (0, 1)]
+                bufs = [torch.full((n + 4096,), 77, dtype=torch.uint8, device="cuda") for n in sizes]
+                loss, lse, rows = sk.entropy_fwd(hd, wd, td, "sum", ws=bufs[0][:sizes[0]])
+                sk.entropy_bwd(hd, wd, td, lse, rows, torch.ones_like(loss), "sum", ws=bufs[1][:sizes[1]])
+                assert all(torch.all(b[n:] == 77) for b, n in zip(bufs, sizes))
+
+
+def test_large_tiles_in_a_captured_graph():
+    """Tiles of 256 (more LDS than a kernel has without asking) recorded and replayed."""
+    T, V, D = 2100, 9000, 256
+    h, w, targets = make(21, T, V, D, torch.bfloat16)
+    hd, wd, td = h.cuda(), w.cuda(), targets.cuda()
+    up = torch.tensor(1.0, device="cuda")
+    l, lse, rows = sk.entropy_fwd(hd, wd, td)
+    want = (l, *sk.entropy_bwd(hd, wd, td, lse, rows, up))
+    check(h, w, targets, "mean", up.cpu(), *want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        l2, lse2, rows2 = sk.entropy_fwd(hd, wd, td)
+        got = (l2, *sk.entropy_bwd(hd, wd, td, lse2, rows2, up))
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        sk.entropy_fwd(hd, wd, td)
+
+
+def test_restored_and_changed_inputs():
+    """Saved tensors that come back from the host give the same gradients; inputs that have changed since are an error."""
+    h, w, targets = make(22, 50, 70, 40, torch.float32)
+    want = run(h, w, targets)
+    a, b, y = h.cuda().requires_grad_(), w.cuda().requires_grad_(), targets.cuda()
+    with torch.autograd.graph.save_on_cpu():
+        loss = ska.linear_cross_entropy(a, b, y)
+    for x, g in zip(torch.autograd.grad(loss, [a, b], want[0].cuda()), want[2:]):
+        assert torch.equal(x, g)
+    for changed in (0, 1, 2):
+        a, b, y = h.cuda().requires_grad_(), w.cuda().requires_grad_(), targets.cuda()
+        loss = ska.linear_cross_entropy(a * 1.0, b * 1.0 if changed != 1 else b, y)
+        hd, wd = a.view(5, 10, 40) * 1.0, b * 1.0
+        loss = ska.linear_cross_entropy(hd, wd, y.view(5, 10))
+        (hd, wd, y)[changed].mul_(1)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            torch.autograd.grad(loss, [a, b])
+
+
+def test_a_second_derivative_is_refused():
+    h, w, targets = make(23, 10, 12, 8, torch.float64)
+    a, b = h.cuda().requires_grad_(), w.cuda().requires_grad_()
+    ga, gb = torch.autograd.grad(ska.linear_cross_entropy(a, b, targets.cuda()) ** 2, [a, b], create_graph=True)
+    with pytest.raises(RuntimeError, match="twice"):
+        (ga.sum() + gb.sum()).backward()
+    t = torch.randn(6, 3, device="cuda", requires_grad=True)
+    (gt,) = torch.autograd.grad((ska.embed(torch.tensor([1, 4], device="cuda"), t) ** 2).sum(), [t], create_graph=True)
+    with pytest.raises(RuntimeError, match="twice"):
+        gt.sum().backward()
+
+
+def test_two_threads_at_once():
+    """Calls from two threads on streams of their own."""
+    import threading
+    sets = [make(30 + i, 90, 400, 64, torch.bfloat16) for i in range(2)]
+    want = [run(*s) for s in sets]
+    got, torch_sync = [None, None], torch.cuda.synchronize
+    torch_sync()
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                got[i] = run(*sets[i])
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x.cpu(), y.cpu()) for x, y in zip(a, b))
+
+
+def test_a_row_alone_and_no_axes():
+    h, w, targets = make(24, 1, 30, 20, torch.float32)
+    targets[0] = 3
+    want = run(h, w, targets, "none")
+    a = h.view(20).cuda().requires_grad_()
+    loss = ska.linear_cross_entropy(a, w.cuda(), targets.view(()).cuda(), "none")
+    (g,) = torch.autograd.grad(loss, [a], want[0].view(()).cuda())
+    assert loss.shape == () and torch.equal(loss, want[1][0]) and torch.equal(g, want[2][0])
