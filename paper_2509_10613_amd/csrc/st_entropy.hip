@@ -66,6 +66,7 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
     auto steps = [&](int64_t n) { return (n + per - 1) / per * per; };
     p.Dp = steps(D);
     p.Tp = steps(T);
+    bool parts = !least;   // (the least workspace has no place for parts)
     auto lay = [&](int64_t piece) {
         p.piece = piece;
         p.pieces = (V + piece - 1) / piece;
@@ -77,8 +78,8 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
             return here;
         };
         p.few = !backward && T <= 16;
-        // (where the logits are few their parts are small; the least workspace has no place for parts)
-        p.logits = choose_tiling(p.size, classes, T, p.Dp / per, p.few || least || T > 65535 || classes * T > (1 << 22) ? 1 : 16, p.sum_size);
+        // (where the logits are few their parts are small)
+        p.logits = choose_tiling(p.size, classes, T, p.Dp / per, p.few || !parts || T > 65535 || classes * T > (1 << 22) ? 1 : 16, p.sum_size);
         p.off_h = take(p.few ? 0 : T * p.Dp, p.size);
         p.off_w = take(p.few ? 0 : piece * p.Dp, p.size);
         p.off_z = take(p.logits.parts > 1 ? p.logits.parts * T * classes : 0, p.sum_size);
@@ -89,8 +90,8 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
             p.off_hit = take(T, p.sum_size);
             p.off_part = take(2 * T * ((piece + p.part_classes - 1) / p.part_classes), p.sum_size);
         } else {
-            p.by_h = choose_tiling(p.size, D, T, (classes + per - 1) / per, least ? 1 : 64, p.sum_size);
-            p.by_w = choose_tiling(p.size, D, classes, p.Tp / per, 1, p.sum_size);
+            p.by_h = choose_tiling(p.size, D, T, (classes + per - 1) / per, parts ? 64 : 1, p.sum_size);
+            p.by_w = choose_tiling(p.size, D, classes, p.Tp / per, parts && classes * D <= 1 << 24 ? 16 : 1, p.sum_size);
             p.sums = p.pieces > 1 || p.by_h.parts > 1;
             p.off_up = take(T + 2, p.sum_size);
             p.off_ht = take(D * p.Tp, p.size);
@@ -98,13 +99,18 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
             p.off_g = take(T * piece, p.size);
             p.off_gt = take(piece * p.Tp, p.size);
             p.off_dh = take(p.sums ? p.by_h.parts * T * D : 0, p.sum_size);
+            p.off_dw = take(p.by_w.parts > 1 ? p.by_w.parts * classes * D : 0, p.sum_size);
         }
         p.total = std::max<size_t>(at, 256);
     };
     const int64_t all = (V + kTileRows - 1) / kTileRows * kTileRows;
-    if (least) {
+    if (least) {   // the smallest pieces, or a single one: then grad_h needs no sums
+        lay(all);
+        const size_t single = p.total;
         lay(kTileRows);
-        return p;
+        if (single < p.total) lay(all);
+        const EntropyPlan best = entropy_plan(backward, T, V, D, dt, false, 0);   // (a few classes: it may take less)
+        return best.total < p.total ? best : p;
     }
     // Pieces of at most 1 GiB of what a class takes, and of those the size for which the compute units' rounds of tiles, over all pieces and products, are
     // fewest: 8192 rows and 4096 channels in pieces of 10240 classes have 640 tiles of grad_w, two and a half rounds that take three.
@@ -146,7 +152,7 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
         best = (all / kTileRows + count - 1) / count;
         if (!fits(best)) best = most;
     }
-    if (!fits(best)) return entropy_plan(backward, T, V, D, dt, true, 0);   // (the smallest pieces without parts: what the least workspace holds)
+    if (!fits(best)) return entropy_plan(backward, T, V, D, dt, true, 0);
     return p;
 }
 

@@ -1159,6 +1159,12 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
         }
         if (grad_w) {
             const Operands o = operands(ht, p.Tp, p.D, gt, p.Tp, n, p.Tp);
+            if (p.by_w.parts > 1) {
+                S* dw = reinterpret_cast<S*>(ws + p.off_dw);
+                if ((e = launch_sums<T>(o, p.by_w, dw, p.D, true, st)) != hipSuccess) return e;
+                ST_TRY((finish_kernel<T><<<blocks_for((n * p.D + 3) / 4), 256, 0, st>>>(dw, p.by_w.parts, n * p.D, scaling, grad_w + first * p.D)));
+                continue;
+            }
             e = with_sub<T>(p.by_w.sub, [&](auto sub) {
                 constexpr int SUB = decltype(sub)::value;
                 return launch_product<T, SUB>(product_kernel<T, SUB, false>, o, 1, st, (S*)nullptr, grad_w + first * p.D, p.D, true, (const S*)scaling);

@@ -56,7 +56,7 @@ struct EntropyPlan {
     size_t off_up;             // backward: every row's upstream gradient (and behind them the scaling, two numbers)
     size_t off_ht, off_wt;     // ... h and a piece of w transposed
     size_t off_g, off_gt;      // ... the piece's gradients of the logits, as they are and transposed
-    size_t off_dh;             // ... the sums of grad_h, one per part
+    size_t off_dh, off_dw;     // ... the sums of grad_h, and of a piece's grad_w, one per part
     size_t total;
 };
 // ws_bytes 0: as fast as it gets; otherwise pieces that fit it.  least: the smallest pieces.

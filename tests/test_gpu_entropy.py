@@ -364,3 +364,11 @@ def test_a_row_alone_and_no_axes():
     loss = ska.linear_cross_entropy(a, w.cuda(), targets.view(()).cuda(), "none")
     (g,) = torch.autograd.grad(loss, [a], want[0].view(()).cuda())
     assert loss.shape == () and torch.equal(loss, want[1][0]) and torch.equal(g, want[2][0])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_few_classes_and_wide_rows(dtype):
+    """Products divided into parts on either side; one piece that takes less than two (several pieces need sums of grad_h)."""
+    for T, V, D in ((1500, 40, 1100), (500, 300, 1030)):
+        h, w, targets = make(T, T, V, D, dtype)
+        check(h, w, targets, "mean", *run(h, w, targets))

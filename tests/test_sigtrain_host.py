@@ -100,6 +100,18 @@ def test_a_piece_fits_every_workspace_from_the_least_on(lib):
             assert ws <= have and piece * pieces >= V and piece * (pieces - 1) < V
 
 
+def test_the_least_workspace_is_never_more_than_the_best(lib):
+    import random
+    rng = random.Random(5)
+    q = lib.sigtrain_entropy_workspace_bytes
+    for _ in range(400):
+        T, V, D = (int(2 ** rng.uniform(0, 14)) for _ in range(3))
+        for back in (0, 1):
+            for dt in range(4):
+                assert 0 < q(back, T, V, D, dt, 1) <= q(back, T, V, D, dt, 0), (back, T, V, D, dt)
+    assert q(1, 2000, 300, 5461, 1, 1) <= q(1, 2000, 300, 5461, 1, 0)
+
+
 def test_describe(lib):
     buf = C.create_string_buffer(256)
     for op in range(4):
