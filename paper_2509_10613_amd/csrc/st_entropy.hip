@@ -94,10 +94,11 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
             p.by_w = choose_tiling(p.size, D, classes, p.Tp / per, parts && classes * D <= 1 << 24 ? 16 : 1, p.sum_size);
             p.sums = p.pieces > 1 || p.by_h.parts > 1;
             p.off_up = take(T + 2, p.sum_size);
-            p.off_ht = take(D * p.Tp, p.size);
-            p.off_wt = take(D * piece, p.size);
-            p.off_g = take(T * piece, p.size);
-            p.off_gt = take(piece * p.Tp, p.size);
+            const bool turned = p.size == 2;   // (the products turn what others need turned copies of)
+            p.off_ht = take(turned ? p.Tp * p.Dp : D * p.Tp, p.size);
+            p.off_wt = take(turned ? per * p.Dp : D * piece, p.size);
+            p.off_g = take((turned ? p.Tp : T) * piece, p.size);
+            p.off_gt = take(turned ? 0 : piece * p.Tp, p.size);
             p.off_dh = take(p.sums ? p.by_h.parts * T * D : 0, p.sum_size);
             p.off_dw = take(p.by_w.parts > 1 ? p.by_w.parts * classes * D : 0, p.sum_size);
         }
@@ -114,7 +115,7 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
     }
     // Pieces of at most 1 GiB of what a class takes, and of those the size for which the compute units' rounds of tiles, over all pieces and products, are
     // fewest: 8192 rows and 4096 channels in pieces of 10240 classes have 640 tiles of grad_w, two and a half rounds that take three.
-    const int64_t each = backward ? 2 * p.Tp * p.size + 2 * p.Dp * p.size : (T <= 16 ? 0 : p.Dp * p.size) + 2 * T * p.sum_size / 64 + 1;
+    const int64_t each = backward ? (p.size == 2 ? 1 : 2) * (p.Tp + p.Dp) * p.size : (T <= 16 ? 0 : p.Dp * p.size) + 2 * T * p.sum_size / 64 + 1;
     int64_t most = ((int64_t)1 << 30) / each / kTileRows;
     if (most < 1) most = 1;
     if (most > (1 << 14)) most = 1 << 14;   // (tiles of a piece are a grid's second index)

@@ -185,12 +185,18 @@ struct Operands {
     int64_t a_pitch, b_pitch;   // bytes between rows
     int64_t m, n;               // rows
     int64_t steps;              // of kStepBytes along k
+    const char* a_tail = nullptr;   // A turned: the last step's rows, if not those behind the others
 };
+using i16x4 = __attribute__((ext_vector_type(4))) short;
+using as3_i16x4 = __attribute__((address_space(3))) i16x4;
 
 // A wave's tile is SUB x SUB tiles of 16 x 16 (2, 4 or 8), a workgroup's twice that on either side.  Large tiles read least from LDS per product: 128 x 128
 // per wave (256 x 256 per workgroup) take 1024 of the 2048 cycles a step's matrix instructions last, and 512 for the loads that arrive.  That is
 // 256 registers of sums (float; double sums take twice as many, so half the tile on either side).
-template <typename T, int SUB>
+// TURN_A, TURN_B (16-bit types): the operand lies with k along its rows, [k][m], and is turned on its way from LDS to the registers, by the reads that
+// hand each of 16 lanes one column of four rows.  Its step is 64 rows of the tile's columns; 32-byte pieces of a row are exchanged by the row's
+// number, so that the 16 rows that one read takes from lie in different banks.
+template <typename T, int SUB, bool TURN_A = false, bool TURN_B = false>
 struct Product {
     using Frag = typename Types<T>::Frag;
     using Acc = typename Types<T>::Acc;
@@ -198,7 +204,13 @@ struct Product {
     static constexpr int kSide = kTile * kStepBytes;           // bytes of one operand's step in LDS
     static constexpr size_t kLds = 4 * kSide;                  // two steps of two operands
     static constexpr int kLoads = kSide / (16 * kThreads);     // 16-byte loads per thread, side and step
-    static_assert(kLoads >= 1 && (SUB <= 4 || sizeof(T) < 8));
+    static_assert(kLoads >= 1 && (SUB <= 4 || sizeof(T) < 8) && (sizeof(T) == 2 || (!TURN_A && !TURN_B)));
+    static constexpr int kRow = kTile * 2, kSlots = kTile / 8;   // a turned row's bytes and 16-byte chunks
+    // what a turned row's pieces are exchanged by: different for eight of rows 8 q .. 8 q + 3 (of two q), beyond what their place in the banks is
+    static __device__ __forceinline__ int mixed(int k)
+    {
+        return kTile == 64 ? (k >> 1 & 1) | (k >> 3 & 1) << 1 : (k & 3) | (k >> 3 & 1) << 2;
+    }
 
     Acc acc[SUB][SUB];
     int lane, wm, wn;
@@ -230,14 +242,20 @@ struct Product {
             for (int j = 0; j < SUB; ++j) acc[i][j] = {0, 0, 0, 0};
         // (32 bits: rows of at most 4 000 000 entries, 256 or, of double, 128 of them)
         uint32_t from_a[kLoads], from_b[kLoads];
-        const char *pa = uniform(o.a + m0 * o.a_pitch), *pb = uniform(o.b + n0 * o.b_pitch);
+        const char *pa = uniform(TURN_A ? o.a : o.a + m0 * o.a_pitch), *pb = uniform(TURN_B ? o.b : o.b + n0 * o.b_pitch);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            // (rows behind the last are read from the last: their results are dropped)
+            // (rows, or columns, behind the last are read from the last: their results are dropped)
             const int row = (i * 4 + w) * 8 + (lane >> 3), c = ((lane & 7) ^ (row & 7)) * 16;
-            from_a[i] = (uint32_t)((m0 + row < o.m ? row : o.m - 1 - m0) * o.a_pitch) + c;
-            from_b[i] = (uint32_t)((n0 + row < o.n ? row : o.n - 1 - n0) * o.b_pitch) + c;
+            const int slot = (i * 4 + w) * 64 + lane, k = slot / kSlots, at = slot % kSlots, col = ((at >> 1) ^ mixed(k)) * 32 + (at & 1) * 16;
+            if constexpr (TURN_A) from_a[i] = (uint32_t)(k * o.a_pitch + (m0 * 2 + col < o.a_pitch ? m0 * 2 + col : o.a_pitch - 16));
+            else from_a[i] = (uint32_t)((m0 + row < o.m ? row : o.m - 1 - m0) * o.a_pitch) + c;
+            if constexpr (TURN_B) from_b[i] = (uint32_t)(k * o.b_pitch + (n0 * 2 + col < o.b_pitch ? n0 * 2 + col : o.b_pitch - 16));
+            else from_b[i] = (uint32_t)((n0 + row < o.n ? row : o.n - 1 - n0) * o.b_pitch) + c;
         }
+        const int64_t step_a = TURN_A ? 64 * o.a_pitch : kStepBytes, step_b = TURN_B ? 64 * o.b_pitch : kStepBytes;
+        int64_t to_send = o.steps;
+        if (TURN_A && to_send == 1 && o.a_tail) pa = uniform(o.a_tail);
         const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + w * 1024;
         // the i-th of a step's loads, A's and B's in turn
         auto send = [&](int half, auto i) {
@@ -246,19 +264,37 @@ struct Product {
             else load<kSide + k * 4096>(pb, from_b[k], base + half * 2 * kSide);
         };
         auto sent = [&] {   // a whole step
-            pa += kStepBytes;
-            pb += kStepBytes;
+            pa += step_a;
+            pb += step_b;
+            if (TURN_A && --to_send == 1 && o.a_tail) pa = uniform(o.a_tail);
         };
         settle(acc);
         Frag fa[2][SUB], fb[2][SUB];
         const int at = (lane & 15) * kStepBytes + (((lane >> 4) ^ (lane & 7)) << 4);
         const char *la = lds + wm * kWave * kStepBytes + at, *lb = lds + kSide + wn * kWave * kStepBytes + at;
+        // a turned operand's: lane 16 q + c asks for row 8 q + c / 4 and the four rows behind, columns 4 (c % 4) .., and gets column c of them
+        const int k0 = (lane >> 4) * 8 + (lane >> 2 & 3), turned = k0 * kRow + (lane & 3) * 8, mix = mixed(k0) << 5;
+        auto turn_read = [&](int side, int which, int kk, int half) {
+            const as3_i16x4* from = (const as3_i16x4*)(lds + half * 2 * kSide + side + kk * 32 * kRow + turned + ((which << 5) ^ mix));
+            union {
+                i16x4 part[2];
+                Frag all;
+            } f;
+            f.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((as3_i16x4*)from);
+            f.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((as3_i16x4*)from + kRow / 2);   // (four rows further on)
+            return f.all;
+        };
         // the i-th of a half step's operands, B's and A's in turn (the second half's chunks are four further on: bit 6 of the address, exchanged
         // or not)
         auto read = [&](int half, int kk, int i) {
             const int to = half * 2 * kSide + i / 2 * 16 * kStepBytes;
-            if (i % 2 == 0) fb[kk][i / 2] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(lb - lds) ^ 64) + to : lb + to);
-            else fa[kk][i / 2] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(la - lds) ^ 64) + to : la + to);
+            if (i % 2 == 0) {
+                if constexpr (TURN_B) fb[kk][i / 2] = turn_read(kSide, wn * SUB + i / 2, kk, half);
+                else fb[kk][i / 2] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(lb - lds) ^ 64) + to : lb + to);
+            } else {
+                if constexpr (TURN_A) fa[kk][i / 2] = turn_read(0, wm * SUB + i / 2, kk, half);
+                else fa[kk][i / 2] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(la - lds) ^ 64) + to : la + to);
+            }
         };
         // Step s in one half of the LDS, s + 1 in the other; more: there is a step s + 2.  One wave per SIMD has to hide every other instruction
         // behind its matrix instructions: one read of LDS or one load after each of them, as written.
@@ -333,29 +369,6 @@ __device__ __forceinline__ int tile_of(const TileOrder& t, int64_t& m, int64_t& 
     m = __builtin_amdgcn_readfirstlane(left / across);
     n = __builtin_amdgcn_readfirstlane(group * kAcross + left % across);
     return __builtin_amdgcn_readfirstlane(place - at * t.parts);
-}
-
-// Four lanes' four numbers turned: lane k of them gets the k-th of each, in the lanes' order.
-template <typename T>
-__device__ __forceinline__ Vec<T, 4> turn(const Vec<T, 4>& v, int lane)
-{
-    static_assert(sizeof(T) == 2);
-    uint32_t d[2];
-    __builtin_memcpy(d, &v, 8);
-    // pairs of lanes: the even one gets the lower halves (its own and the other's), the odd one the upper
-    uint32_t p[2], q[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t other = __builtin_amdgcn_mov_dpp(d[i], 0xb1, 0xf, 0xf, true);   // lane ^ 1
-        // v_perm's bytes 4 .. 7 are its first operand's
-        p[i] = lane & 1 ? __builtin_amdgcn_perm(d[i], other, 0x07060302u) : __builtin_amdgcn_perm(other, d[i], 0x05040100u);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) q[i] = __builtin_amdgcn_mov_dpp(p[i], 0x4e, 0xf, 0xf, true);   // lane ^ 2
-    const uint32_t r[2] = {lane & 2 ? q[1] : p[0], lane & 2 ? p[1] : q[0]};
-    Vec<T, 4> t;
-    __builtin_memcpy(&t, r, 8);
-    return t;
 }
 
 // Results of 16 bits leave through LDS, as whole rows of the tile: straight from the registers a store takes 32 bytes each of 16 rows, and the
@@ -609,8 +622,9 @@ __global__ __launch_bounds__(kThreads) void parts_grads_kernel(const typename Ty
             v = u != 0 ? (T)(u * p) : T(0);
         }
         tile[i / N][i % N] = v;
-        if (row < rows && cls < g_pitch) g[row * g_pitch + cls] = v;
+        if (row < (sizeof(T) == 2 ? gt_pitch : rows) && cls < g_pitch) g[row * g_pitch + cls] = v;
     }
+    if constexpr (sizeof(T) == 2) return;
     __syncthreads();
     for (int i = threadIdx.x; i < N * N; i += kThreads) {
         const int64_t row = r0 + i % N, cls = c0 + i / N;
@@ -618,7 +632,8 @@ __global__ __launch_bounds__(kThreads) void parts_grads_kernel(const typename Ty
     }
 }
 
-// Backward: the gradients of the piece's logits, g[row][class] and gt[class][row], zeros up to whole steps.
+// Backward: the gradients of the piece's logits, g[row][class] with zeros up to whole steps; of 16-bit types also zeros in the rows up to whole steps
+// (`gt_pitch` of them), of others gt[class][row], the same turned.
 template <typename T, int SUB>
 __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void grads_kernel(Operands o, TileOrder order, const void* targets, int it, int64_t first_class,
                                                          const typename Types<T>::Sum* lse, const typename Types<T>::Sum* up, T* g,
@@ -637,7 +652,6 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void grads_kernel(Opera
     const int lane = p.lane, wm = p.wm, wn = p.wn;
     const bool inside = m0 + kTile <= o.m;
     const OutboxOf<T, kTile> outbox{lds};
-    Vec<T, 4> kept[sizeof(T) == 2 ? SUB : 1][sizeof(T) == 2 ? SUB : 1];
 #pragma unroll
     for (int j = 0; j < SUB; ++j) {
         const int64_t row = n0 + wn * kWave + j * 16 + (lane & 15);
@@ -665,7 +679,6 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void grads_kernel(Opera
 #pragma unroll
             for (int r = 0; r < 4; ++r) v.v[r] = (T)(some ? x[r] : (S)0);   // rows without a target stay 0 whatever their logits are
             if constexpr (sizeof(T) == 2) {
-                kept[i][j] = v;   // (of f16 and bf16)
                 outbox.put(wn * kWave + j * 16 + (lane & 15), wm * kWave + i * 16 + acc_row<T>(lane, 0), v);
                 continue;
             }
@@ -680,25 +693,18 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void grads_kernel(Opera
         }
     }
     if constexpr (sizeof(T) == 2) {
-        outbox.send(g + n0 * g_pitch + m0, g_pitch, o.n - n0, g_pitch - m0);
-        // four lanes hold four classes of four rows, and each takes one class of the four rows
-#pragma unroll
-        for (int j = 0; j < SUB; ++j)
-#pragma unroll
-            for (int i = 0; i < SUB; ++i)
-                outbox.put(wm * kWave + i * 16 + acc_row<T>(lane, 0) + (lane & 3), wn * kWave + j * 16 + (lane & 12), turn(kept[i][j], lane));
-        outbox.send(gt + m0 * gt_pitch + n0, gt_pitch, o.m - m0, gt_pitch - n0);
+        outbox.send(g + n0 * g_pitch + m0, g_pitch, gt_pitch - n0, g_pitch - m0);
     }
 }
 
 // out[n][m] (pitch D) = the products times *unscale, rounded; or, with SUMS, sum[part][n][m] = the products over the part's steps, added to
 // what is there unless `first`.  parts: the steps are divided among this many workgroups per tile.
-template <typename T, int SUB, bool SUMS>
+template <typename T, int SUB, bool SUMS, bool TURN_A, bool TURN_B>
 __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Operands o, TileOrder order, typename Types<T>::Sum* sum, T* out, int64_t D, bool first,
                                                               const typename Types<T>::Sum* unscale)
 {
     using S = typename Types<T>::Sum;
-    using P = Product<T, SUB>;
+    using P = Product<T, SUB, TURN_A, TURN_B>;
     constexpr int kTile = P::kTile, kWave = P::kWave;
     extern __shared__ __align__(16) char lds[];
     int64_t tile_m, tile_n;
@@ -706,8 +712,9 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Ope
     const int64_t m0 = tile_m * kTile, n0 = tile_n * kTile;
     if constexpr (SUMS) {
         const int64_t from = o.steps * part / order.parts, to = o.steps * (part + 1) / order.parts;
-        o.a += from * kStepBytes;
-        o.b += from * kStepBytes;
+        o.a += from * (TURN_A ? 64 * o.a_pitch : kStepBytes);
+        o.b += from * (TURN_B ? 64 * o.b_pitch : kStepBytes);
+        if (to < o.steps) o.a_tail = nullptr;
         o.steps = to - from;
         sum += part * o.n * D;
     }
@@ -784,17 +791,22 @@ __global__ __launch_bounds__(256) void finish_kernel(const typename Types<T>::Su
 }
 
 // ------------------------------------------------------------------------------------------------ copies
-// dst[rows][pitch] = src[rows][cols], zeros behind the columns.
+// dst[all][pitch] = src[rows][cols], zeros behind the columns and the rows.  targets not null: rows without one are zeros, whatever they hold.
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(const T* src, T* dst, int64_t rows, int64_t cols, int64_t pitch)
+__global__ __launch_bounds__(256) void pack_kernel(const T* src, T* dst, int64_t rows, int64_t all, int64_t cols, int64_t pitch, const void* targets,
+                                                   int it, int64_t V)
 {
     constexpr int E = kPer16<T>;
-    const int64_t per_row = pitch / E, items = rows * per_row;
+    const int64_t per_row = pitch / E, items = all * per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / per_row, col = (i - row * per_row) * E;
-        const int64_t left = cols - col;
-        const Vec<T, E> v = left >= E ? load_vec<T, E>(src + row * cols + col) : load_some<T, E>(src + row * cols + col, (int)(left > 0 ? left : 0));
-        store_vec(dst + row * pitch + col, v);
+        int64_t left = row < rows ? cols - col : 0;
+        if (targets && row < rows) {
+            const int64_t t = load_index(targets, row, it);
+            if (t < 0 || t >= V) left = 0;
+        }
+        const T* from = src + row * cols + col;
+        store_vec(dst + row * pitch + col, left >= E ? load_vec<T, E>(from) : load_some<T, E>(from, (int)(left > 0 ? left : 0)));
     }
 }
 
@@ -1003,14 +1015,14 @@ unsigned blocks_for(int64_t items) { return (unsigned)((items + 255) / 256 < 163
         if (err_ != hipSuccess) return err_;       \
     } while (0)
 
-// A matrix with rows in whole steps: the caller's, or a copy.
+// A matrix with rows in whole steps: the caller's, or a copy, with zeros in the rows up to `all`.
 template <typename T>
-hipError_t in_steps(const T* src, int64_t rows, int64_t cols, int64_t pitch, void* copy, const T** out, hipStream_t st)
+hipError_t in_steps(const T* src, int64_t rows, int64_t all, int64_t cols, int64_t pitch, void* copy, const T** out, hipStream_t st)
 {
     *out = src;
     if (cols == pitch && reinterpret_cast<uintptr_t>(src) % 16 == 0) return hipSuccess;
     *out = static_cast<const T*>(copy);
-    ST_TRY((pack_kernel<T><<<blocks_for(rows * (pitch / kPer16<T>)), 256, 0, st>>>(src, static_cast<T*>(copy), rows, cols, pitch)));
+    ST_TRY((pack_kernel<T><<<blocks_for(all * (pitch / kPer16<T>)), 256, 0, st>>>(src, static_cast<T*>(copy), rows, all, cols, pitch, nullptr, 0, 0)));
     return hipSuccess;
 }
 
@@ -1042,12 +1054,12 @@ hipError_t launch_product(K kernel, const Operands& o, int parts, hipStream_t st
     kernel<<<t.tiles_m * t.tiles_n * t.parts, kThreads, P::kLds, st>>>(o, t, args...);
     return hipGetLastError();
 }
-template <typename T>
+template <typename T, bool TURN_A = false, bool TURN_B = false>
 hipError_t launch_sums(const Operands& o, Tiling t, typename Types<T>::Sum* sum, int64_t pitch, bool first, hipStream_t st)
 {
     return with_sub<T>(t.sub, [&](auto sub) {
         constexpr int SUB = decltype(sub)::value;
-        return launch_product<T, SUB>(product_kernel<T, SUB, true>, o, t.parts, st, sum, (T*)nullptr, pitch, first,
+        return launch_product<T, SUB>(product_kernel<T, SUB, true, TURN_A, TURN_B>, o, t.parts, st, sum, (T*)nullptr, pitch, first,
                                       (const typename Types<T>::Sum*)nullptr);
     });
 }
@@ -1068,7 +1080,7 @@ hipError_t entropy_run_fwd(const EntropyPlan& p, const T* h, const T* w, const v
     S *part_max = reinterpret_cast<S*>(ws + p.off_part), *part_sum = part_max + most * p.T;
     const T* hs = h;
     hipError_t e = hipSuccess;
-    if (!p.few && (e = in_steps(h, p.T, p.D, p.Dp, ws + p.off_h, &hs, st)) != hipSuccess) return e;
+    if (!p.few && (e = in_steps(h, p.T, p.T, p.D, p.Dp, ws + p.off_h, &hs, st)) != hipSuccess) return e;
     // (the running maxima are dead where the losses of the rows are written: a thread reads its own first)
     S* losses = reduction == ST_NONE ? static_cast<S*>(loss) : run_max;
     for (int64_t i = 0; i < p.pieces; ++i) {
@@ -1078,7 +1090,7 @@ hipError_t entropy_run_fwd(const EntropyPlan& p, const T* h, const T* w, const v
                                                                             part_sum, hit)));
         } else {
             const T* wsrc;
-            if ((e = in_steps(w + first * p.D, n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
+            if ((e = in_steps(w + first * p.D, n, n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
             const Operands o = operands(wsrc, p.Dp, n, hs, p.Dp, p.T, p.Dp);
             if (p.logits.parts > 1) {
                 S* z = reinterpret_cast<S*>(ws + p.off_z);
@@ -1115,23 +1127,27 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
         return hipSuccess;
     }
     S *up = reinterpret_cast<S*>(ws + p.off_up), *scaling = up + p.T, *dh = reinterpret_cast<S*>(ws + p.off_dh);
+    // 16-bit types: g, w and h are turned on their way to the registers; others: copies of them are
+    constexpr bool kTurned = sizeof(T) == 2;
     T *ht = reinterpret_cast<T*>(ws + p.off_ht), *wt = reinterpret_cast<T*>(ws + p.off_wt);
     T *g = reinterpret_cast<T*>(ws + p.off_g), *gt = reinterpret_cast<T*>(ws + p.off_gt);
     ST_TRY((upstream_kernel<T><<<1, 1024, 0, st>>>(static_cast<const S*>(grad), targets, it, p.T, p.V, reduction, rows, up, scaling)));
     const T* hs;
-    hipError_t e = in_steps(h, p.T, p.D, p.Dp, ws + p.off_h, &hs, st);
+    hipError_t e = in_steps(h, p.T, p.T, p.D, p.Dp, ws + p.off_h, &hs, st);
     if (e != hipSuccess) return e;
     auto turn = [&](const T* src, T* dst, int64_t r, int64_t pitch, const void* only) -> hipError_t {
         const dim3 grid((unsigned)((pitch + 63) / 64), (unsigned)((p.D + kTurnCols<T> - 1) / kTurnCols<T>));
         ST_TRY((transpose_kernel<T><<<grid, 256, 0, st>>>(src, dst, r, p.D, pitch, only, it, p.V)));
         return hipSuccess;
     };
-    if (grad_w && (e = turn(h, ht, p.T, p.Tp, targets)) != hipSuccess) return e;
+    if (grad_w && !kTurned && (e = turn(h, ht, p.T, p.Tp, targets)) != hipSuccess) return e;
+    if (grad_w && kTurned)
+        ST_TRY((pack_kernel<T><<<blocks_for(p.Tp * (p.Dp / kPer16<T>)), 256, 0, st>>>(h, ht, p.T, p.Tp, p.D, p.Dp, targets, it, p.V)));
     for (int64_t i = 0; i < p.pieces; ++i) {
         const int64_t first = i * p.piece, n = p.V - first < p.piece ? p.V - first : p.piece;
         const int64_t per = kStepBytes / (int64_t)sizeof(T), np = (n + per - 1) / per * per;
         const T* wsrc;
-        if ((e = in_steps(w + first * p.D, n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
+        if ((e = in_steps(w + first * p.D, n, kTurned ? np : n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
         const Operands logits = operands(wsrc, p.Dp, n, hs, p.Dp, p.T, p.Dp);
         if (p.logits.parts > 1) {
             S* z = reinterpret_cast<S*>(ws + p.off_z);
@@ -1147,27 +1163,39 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
             if (e != hipSuccess) return e;
         }
         if (grad_h) {
-            if ((e = turn(w + first * p.D, wt, n, np, nullptr)) != hipSuccess) return e;
-            const Operands o = operands(wt, np, p.D, g, np, p.T, np);
-            if (p.sums) e = launch_sums<T>(o, p.by_h, dh, p.D, i == 0, st);
+            Operands o;
+            if constexpr (kTurned) {
+                o = operands(wsrc, p.Dp, p.D, g, np, p.T, np);
+                if (wsrc == w + first * p.D && n != np) {   // (behind the caller's last row nothing may be read)
+                    o.a_tail = reinterpret_cast<const char*>(wt);
+                    const int64_t whole = np - per;
+                    ST_TRY((pack_kernel<T><<<blocks_for(per * (p.Dp / kPer16<T>)), 256, 0, st>>>(wsrc + whole * p.Dp, wt, n - whole, per, p.D, p.Dp, nullptr, 0,
+                                                                                               0)));
+                }
+            } else {
+                if ((e = turn(w + first * p.D, wt, n, np, nullptr)) != hipSuccess) return e;
+                o = operands(wt, np, p.D, g, np, p.T, np);
+            }
+            if (p.sums) e = launch_sums<T, kTurned, false>(o, p.by_h, dh, p.D, i == 0, st);
             else
                 e = with_sub<T>(p.by_h.sub, [&](auto sub) {
                     constexpr int SUB = decltype(sub)::value;
-                    return launch_product<T, SUB>(product_kernel<T, SUB, false>, o, 1, st, (S*)nullptr, grad_h, p.D, true, (const S*)scaling);
+                    return launch_product<T, SUB>(product_kernel<T, SUB, false, kTurned, false>, o, 1, st, (S*)nullptr, grad_h, p.D, true, (const S*)scaling);
                 });
             if (e != hipSuccess) return e;
         }
         if (grad_w) {
-            const Operands o = operands(ht, p.Tp, p.D, gt, p.Tp, n, p.Tp);
+            const Operands o = kTurned ? operands(ht, p.Dp, p.D, g, np, n, p.Tp) : operands(ht, p.Tp, p.D, gt, p.Tp, n, p.Tp);
             if (p.by_w.parts > 1) {
                 S* dw = reinterpret_cast<S*>(ws + p.off_dw);
-                if ((e = launch_sums<T>(o, p.by_w, dw, p.D, true, st)) != hipSuccess) return e;
+                if ((e = launch_sums<T, kTurned, kTurned>(o, p.by_w, dw, p.D, true, st)) != hipSuccess) return e;
                 ST_TRY((finish_kernel<T><<<blocks_for((n * p.D + 3) / 4), 256, 0, st>>>(dw, p.by_w.parts, n * p.D, scaling, grad_w + first * p.D)));
                 continue;
             }
             e = with_sub<T>(p.by_w.sub, [&](auto sub) {
                 constexpr int SUB = decltype(sub)::value;
-                return launch_product<T, SUB>(product_kernel<T, SUB, false>, o, 1, st, (S*)nullptr, grad_w + first * p.D, p.D, true, (const S*)scaling);
+                return launch_product<T, SUB>(product_kernel<T, SUB, false, kTurned, kTurned>, o, 1, st, (S*)nullptr, grad_w + first * p.D, p.D, true,
+                                              (const S*)scaling);
             });
             if (e != hipSuccess) return e;
         }
