@@ -23,7 +23,7 @@ Tiling choose_tiling(int size, int64_t m, int64_t n, int64_t steps, int64_t most
 {
     Tiling best{};
     double least = 1e300;
-    for (int sub = size == 8 ? 4 : 8; sub >= 2; sub /= 2) {
+    for (int sub = size == 2 ? 8 : 4; sub >= 2; sub /= 2) {
         const int64_t tile = 32 * sub, tiles = ((m + tile - 1) / tile) * ((n + tile - 1) / tile);
         const double busy = sub * sub * (size == 2 ? 43.0 : 270.0), fed = sub * 205.0 + 100.0;
         for (int64_t parts = 1; parts <= most_parts && (parts == 1 || steps / parts >= 8); parts *= 2) {
@@ -134,7 +134,7 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
     }
     int64_t best = most;
     if (backward && most < all / kTileRows) {
-        const int64_t tile = p.size == 8 ? 128 : 256, units = 256, per_row = kTileRows / tile;
+        const int64_t tile = p.size == 2 ? 256 : 128, units = 256, per_row = kTileRows / tile;
         const int64_t tt = (T + tile - 1) / tile, td = (D + tile - 1) / tile;
         auto rounds = [&](int64_t tiles) { return (double)((tiles + units - 1) / units); };
         double least_cost = 1e300;
