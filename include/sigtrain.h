@@ -56,8 +56,9 @@ enum { ST_NONE = 0, ST_MEAN = 1, ST_SUM = 2 };
  * Products are summed in float (double for ST_F64), and logits are never rounded to fewer bits.
  *
  * Backward: `grad` is dF/dloss, shaped and typed as `loss`; lse and rows are the forward call's.  grad_h[T, D] and grad_w[V, D]
- * (either may be NULL).  The logits' gradients u_t (exp(z - lse) - [v = target]) of a piece of the classes are rounded to the arrays' type
- * before they are multiplied by w and h (for ST_F16 after a scaling by a power of two that keeps them in range).
+ * (either may be NULL).  The logits' gradients u_t (exp(z - lse) - [v = target]) of a piece of the classes are rounded to the arrays' type before they
+ * are multiplied by w and h: divided by the largest |u_t| (the mean's and the sum's common factor, which 16-bit types need not hold), for ST_F16
+ * times 2^14, so that small probabilities stay in its range; the products are multiplied by that again, in the sums' type.
  *
  * The workspace query gives what the call is fastest with; with `least` set, what it takes (smaller pieces).
  */

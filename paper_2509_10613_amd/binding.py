@@ -410,6 +410,8 @@ _ST_REDUCTIONS = {"none": ST_NONE, "mean": ST_MEAN, "sum": ST_SUM}
 
 
 def _st_dt(t):
+    if t.is_neg():
+        raise ValueError("a lazily negated tensor: call resolve_neg() first")
     try:
         return _ST_TYPES[t.dtype]
     except KeyError:

@@ -231,6 +231,14 @@ struct Product {
                      : "memory", "scc", "m0");
     }
 
+    // (the instruction alone does not keep the compiler from moving reads of LDS over it)
+    static __device__ __forceinline__ void barrier()
+    {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
     // The tile with rows m0.. of A and n0.. of B.  A step's operands lie in LDS as rows of 128 bytes, the 16-byte chunks of a row exchanged by
     // its number modulo 8, so that eight rows' chunks of one column lie in different banks.  Two steps are under way: a wave reads the second half
     // of step s, multiplies the first half, and after the one barrier of a step (everybody has read step s, step s + 1 has arrived) sends for
@@ -315,8 +323,7 @@ struct Product {
             });
             if constexpr (kNext) {
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
-                __builtin_amdgcn_s_barrier();
-                __builtin_amdgcn_sched_barrier(0);
+                barrier();
             }
             unroll<SUB>([&](auto i) {
                 Types<T>::products(fa[1][i], fb[1], acc[i], [&](int j) {
@@ -341,7 +348,7 @@ struct Product {
         } else {
             asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         }
-        __builtin_amdgcn_s_barrier();
+        barrier();
 #pragma unroll
         for (int i = 0; i < 2 * SUB; ++i) read(0, 0, i);
         int half = 0;
