@@ -189,6 +189,8 @@ struct Operands {
     int64_t m, n;               // rows
     int64_t steps;              // of kStepBytes along k
     const char* a_tail = nullptr;   // A turned: the last step's rows, if not those behind the others
+    const char* a_zero = nullptr;   // A not turned: where 16 zeros are, if its rows end within the last step
+    int a_left = 0;                 // ... and how many bytes of that step they have, a multiple of 16
 };
 using i16x4 = __attribute__((ext_vector_type(4))) short;
 using as3_i16x4 = __attribute__((address_space(3))) i16x4;
@@ -229,6 +231,13 @@ struct Product {
                      :
                      : "s"(to), "n"(PAST), "v"(offset), "s"(base)
                      : "memory", "scc", "m0");
+    }
+
+    // ... at an address of each lane's own
+    template <int PAST>
+    static __device__ __forceinline__ void load_at(const char* from, uint32_t to)
+    {
+        asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off" : : "s"(to), "n"(PAST), "v"(from) : "memory", "scc", "m0");
     }
 
     // (the instruction alone does not keep the compiler from moving reads of LDS over it)
@@ -276,6 +285,13 @@ struct Product {
             if constexpr (decltype(i)::value % 2 == 0) load<k * 4096>(pa, from_a[k], base + half * 2 * kSide);
             else load<kSide + k * 4096>(pb, from_b[k], base + half * 2 * kSide);
         };
+        // ... of the last step where A's rows end within it: zeros behind them (what lies there may be infinite, or nobody's)
+        const bool ends = ((lane & 7) ^ (lane >> 3)) * 16 >= o.a_left;
+        auto send_end = [&](int half, auto i) {
+            constexpr int k = decltype(i)::value / 2;
+            if constexpr (decltype(i)::value % 2 == 0) load_at<k * 4096>(ends ? o.a_zero : pa + from_a[k], base + half * 2 * kSide);
+            else send(half, i);
+        };
         auto sent = [&] {   // a whole step
             pa += step_a;
             pb += step_b;
@@ -309,10 +325,11 @@ struct Product {
                 else fa[kk][i / 2] = *reinterpret_cast<const Frag*>(kk ? lds + ((uintptr_t)(la - lds) ^ 64) + to : la + to);
             }
         };
-        // Step s in one half of the LDS, s + 1 in the other; more: there is a step s + 2.  One wave per SIMD has to hide every other instruction
+        // Step s in one half of the LDS, s + 1 in the other; more: 1 if there is a step s + 2, 2 if that is one where A's rows end.  One wave per SIMD has to hide every other instruction
         // behind its matrix instructions: one read of LDS or one load after each of them, as written.
         auto step = [&](int half, auto next, auto more) {
-            constexpr bool kNext = decltype(next)::value, kMore = decltype(more)::value;
+            constexpr bool kNext = decltype(next)::value;
+            constexpr int kMore = decltype(more)::value;
             constexpr int kAll = SUB * SUB, kEvery = SUB == 8 ? 2 : 1;
             unroll<SUB>([&](auto i) {
                 Types<T>::products(fa[0][i], fb[0], acc[i], [&](int j) {
@@ -329,21 +346,31 @@ struct Product {
                 Types<T>::products(fa[1][i], fb[1], acc[i], [&](int j) {
                     const int at = i * SUB + j;
                     if (kNext && at % kEvery == 0 && at / kEvery < 2 * SUB) read(half ^ 1, 0, at / kEvery);
-                    if constexpr (kMore)
+                    if constexpr (kMore != 0)
                         unroll<2 * kLoads>([&](auto l) {
-                            if (at == l * kEvery + kEvery - 1) send(half, l);
+                            if (at != l * kEvery + kEvery - 1) return;
+                            if constexpr (kMore == 2) send_end(half, l);
+                            else send(half, l);
                         });
                     __builtin_amdgcn_sched_barrier(0);
                 });
             });
             static_assert(2 * SUB * kEvery <= kAll && 2 * kLoads * kEvery <= kAll);
-            if constexpr (kMore) sent();
+            if constexpr (kMore != 0) sent();
         };
-        unroll<2 * kLoads>([&](auto i) { send(0, i); });
-        sent();
-        if (o.steps > 1) {
-            unroll<2 * kLoads>([&](auto i) { send(1, i); });
+        using Yes = std::true_type;
+        const bool end = !TURN_A && o.a_zero != nullptr;
+        auto send_first = [&](int half) {   // the first step, or the second
+            if (end && o.steps == half + 1) {
+                if constexpr (!TURN_A) unroll<2 * kLoads>([&](auto i) { send_end(half, i); });
+            } else {
+                unroll<2 * kLoads>([&](auto i) { send(half, i); });
+            }
             sent();
+        };
+        send_first(0);
+        if (o.steps > 1) {
+            send_first(1);
             asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * kLoads) : "memory");
         } else {
             asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
@@ -352,15 +379,21 @@ struct Product {
 #pragma unroll
         for (int i = 0; i < 2 * SUB; ++i) read(0, 0, i);
         int half = 0;
-        for (int64_t s = 2; s < o.steps; ++s) {
-            step(half, std::true_type{}, std::true_type{});
+        const int64_t whole = o.steps - (end ? 1 : 0);
+        for (int64_t s = 2; s < whole; ++s) {
+            step(half, Yes{}, std::integral_constant<int, 1>{});
             half ^= 1;
         }
+        if constexpr (!TURN_A)
+            if (end && o.steps > 2) {
+                step(half, Yes{}, std::integral_constant<int, 2>{});
+                half ^= 1;
+            }
         if (o.steps > 1) {
-            step(half, std::true_type{}, std::false_type{});
+            step(half, Yes{}, std::integral_constant<int, 0>{});
             half ^= 1;
         }
-        step(half, std::false_type{}, std::false_type{});
+        step(half, std::false_type{}, std::integral_constant<int, 0>{});
         settle(acc);
         __syncthreads();   // (what follows may use the LDS)
     }
@@ -726,7 +759,7 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Ope
         const int64_t from = o.steps * part / order.parts, to = o.steps * (part + 1) / order.parts;
         o.a += from * (TURN_A ? 64 * o.a_pitch : kStepBytes);
         o.b += from * (TURN_B ? 64 * o.b_pitch : kStepBytes);
-        if (to < o.steps) o.a_tail = nullptr;
+        if (to < o.steps) o.a_tail = o.a_zero = nullptr;
         o.steps = to - from;
         sum += part * o.n * D;
     }
@@ -1027,15 +1060,31 @@ unsigned blocks_for(int64_t items) { return (unsigned)((items + 255) / 256 < 163
         if (err_ != hipSuccess) return err_;       \
     } while (0)
 
-// A matrix with rows in whole steps: the caller's, or a copy, with zeros in the rows up to `all`.
+// A matrix with rows in whole steps: the caller's, or a copy, with zeros in the rows up to `all`.  pitch: in whole steps; what comes back may also be the
+// caller's with rows of whole 16 bytes (`ends`: the products that read it take zeros for what is behind them).
 template <typename T>
-hipError_t in_steps(const T* src, int64_t rows, int64_t all, int64_t cols, int64_t pitch, void* copy, const T** out, hipStream_t st)
+hipError_t in_steps(const T* src, int64_t rows, int64_t all, int64_t cols, int64_t* pitch, void* copy, const T** out, bool ends, hipStream_t st)
 {
     *out = src;
-    if (cols == pitch && reinterpret_cast<uintptr_t>(src) % 16 == 0) return hipSuccess;
+    if ((cols == *pitch || (ends && cols % kPer16<T> == 0)) && reinterpret_cast<uintptr_t>(src) % 16 == 0) {
+        *pitch = cols;
+        return hipSuccess;
+    }
     *out = static_cast<const T*>(copy);
-    ST_TRY((pack_kernel<T><<<blocks_for(all * (pitch / kPer16<T>)), 256, 0, st>>>(src, static_cast<T*>(copy), rows, all, cols, pitch, nullptr, 0, 0)));
+    ST_TRY((pack_kernel<T><<<blocks_for(all * (*pitch / kPer16<T>)), 256, 0, st>>>(src, static_cast<T*>(copy), rows, all, cols, *pitch, nullptr, 0, 0)));
     return hipSuccess;
+}
+// The logits' operands: classes of w, in rows of `pitch`, and h in whole steps (whose first row, where D is none, has zeros behind it).
+template <typename T>
+Operands logits_of(const T* w, int64_t pitch, int64_t n, const T* hs, const EntropyPlan& p)
+{
+    Operands o{reinterpret_cast<const char*>(w), reinterpret_cast<const char*>(hs), pitch * (int64_t)sizeof(T), p.Dp * (int64_t)sizeof(T), n, p.T,
+               p.Dp * (int64_t)sizeof(T) / kStepBytes};
+    if (pitch != p.Dp) {
+        o.a_zero = reinterpret_cast<const char*>(hs + p.D);
+        o.a_left = (int)(p.D * (int64_t)sizeof(T) % kStepBytes);
+    }
+    return o;
 }
 
 template <typename T>
@@ -1092,7 +1141,8 @@ hipError_t entropy_run_fwd(const EntropyPlan& p, const T* h, const T* w, const v
     S *part_max = reinterpret_cast<S*>(ws + p.off_part), *part_sum = part_max + most * p.T;
     const T* hs = h;
     hipError_t e = hipSuccess;
-    if (!p.few && (e = in_steps(h, p.T, p.T, p.D, p.Dp, ws + p.off_h, &hs, st)) != hipSuccess) return e;
+    int64_t h_pitch = p.Dp;
+    if (!p.few && (e = in_steps(h, p.T, p.T, p.D, &h_pitch, ws + p.off_h, &hs, false, st)) != hipSuccess) return e;
     // (the running maxima are dead where the losses of the rows are written: a thread reads its own first)
     S* losses = reduction == ST_NONE ? static_cast<S*>(loss) : run_max;
     for (int64_t i = 0; i < p.pieces; ++i) {
@@ -1102,8 +1152,9 @@ hipError_t entropy_run_fwd(const EntropyPlan& p, const T* h, const T* w, const v
                                                                             part_sum, hit)));
         } else {
             const T* wsrc;
-            if ((e = in_steps(w + first * p.D, n, n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
-            const Operands o = operands(wsrc, p.Dp, n, hs, p.Dp, p.T, p.Dp);
+            int64_t pitch = p.Dp;
+            if ((e = in_steps(w + first * p.D, n, n, p.D, &pitch, ws + p.off_w, &wsrc, true, st)) != hipSuccess) return e;
+            const Operands o = logits_of(wsrc, pitch, n, hs, p);
             if (p.logits.parts > 1) {
                 S* z = reinterpret_cast<S*>(ws + p.off_z);
                 if ((e = launch_sums<T>(o, p.logits, z, n, true, st)) != hipSuccess) return e;
@@ -1145,7 +1196,8 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
     T *g = reinterpret_cast<T*>(ws + p.off_g), *gt = reinterpret_cast<T*>(ws + p.off_gt);
     ST_TRY((upstream_kernel<T><<<1, 1024, 0, st>>>(static_cast<const S*>(grad), targets, it, p.T, p.V, reduction, rows, up, scaling)));
     const T* hs;
-    hipError_t e = in_steps(h, p.T, p.T, p.D, p.Dp, ws + p.off_h, &hs, st);
+    int64_t h_pitch = p.Dp;
+    hipError_t e = in_steps(h, p.T, p.T, p.D, &h_pitch, ws + p.off_h, &hs, false, st);
     if (e != hipSuccess) return e;
     auto turn = [&](const T* src, T* dst, int64_t r, int64_t pitch, const void* only) -> hipError_t {
         const dim3 grid((unsigned)((pitch + 63) / 64), (unsigned)((p.D + kTurnCols<T> - 1) / kTurnCols<T>));
@@ -1159,8 +1211,9 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
         const int64_t first = i * p.piece, n = p.V - first < p.piece ? p.V - first : p.piece;
         const int64_t per = kStepBytes / (int64_t)sizeof(T), np = (n + per - 1) / per * per;
         const T* wsrc;
-        if ((e = in_steps(w + first * p.D, n, kTurned ? np : n, p.D, p.Dp, ws + p.off_w, &wsrc, st)) != hipSuccess) return e;
-        const Operands logits = operands(wsrc, p.Dp, n, hs, p.Dp, p.T, p.Dp);
+        int64_t pitch = p.Dp;
+        if ((e = in_steps(w + first * p.D, n, kTurned ? np : n, p.D, &pitch, ws + p.off_w, &wsrc, true, st)) != hipSuccess) return e;
+        const Operands logits = logits_of(wsrc, pitch, n, hs, p);
         if (p.logits.parts > 1) {
             S* z = reinterpret_cast<S*>(ws + p.off_z);
             if ((e = launch_sums<T>(logits, p.logits, z, n, true, st)) != hipSuccess) return e;
@@ -1177,12 +1230,12 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
         if (grad_h) {
             Operands o;
             if constexpr (kTurned) {
-                o = operands(wsrc, p.Dp, p.D, g, np, p.T, np);
+                o = operands(wsrc, pitch, p.D, g, np, p.T, np);
                 if (wsrc == w + first * p.D && n != np) {   // (behind the caller's last row nothing may be read)
                     o.a_tail = reinterpret_cast<const char*>(wt);
                     const int64_t whole = np - per;
-                    ST_TRY((pack_kernel<T><<<blocks_for(per * (p.Dp / kPer16<T>)), 256, 0, st>>>(wsrc + whole * p.Dp, wt, n - whole, per, p.D, p.Dp, nullptr, 0,
-                                                                                               0)));
+                    ST_TRY((pack_kernel<T><<<blocks_for(per * (pitch / kPer16<T>)), 256, 0, st>>>(wsrc + whole * pitch, wt, n - whole, per, p.D, pitch, nullptr,
+                                                                                                0, 0)));
                 }
             } else {
                 if ((e = turn(w + first * p.D, wt, n, np, nullptr)) != hipSuccess) return e;

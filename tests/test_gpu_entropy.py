@@ -372,3 +372,32 @@ def test_few_classes_and_wide_rows(dtype):
     for T, V, D in ((1500, 40, 1100), (500, 300, 1030)):
         h, w, targets = make(T, T, V, D, dtype)
         check(h, w, targets, "mean", *run(h, w, targets))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V,D", [(70, 90, 8), (70, 90, 72), (130, 300, 200), (40, 257, 1992), (600, 700, 136)])
+def test_rows_that_end_within_a_step(T, V, D, dtype):
+    """Rows of whole 16 bytes that are read as they lie: what is behind a row's end, here a class that is masked by minus infinity, stays out of it."""
+    h, w, targets = make(T + D, T, V, D, dtype)
+    h[:, 0] = h[:, 0].abs() + 0.5
+    masked = torch.arange(5, V, 7)
+    keep = torch.ones(V, dtype=torch.bool)
+    keep[masked] = False
+    targets = torch.where((targets >= 0) & (targets < V) & ~keep[targets.clamp(0, V - 1)], 0, targets)
+    clean = torch.cumsum(keep, 0) - 1                       # the classes that are left, by number
+    few = torch.where((targets >= 0) & (targets < V), clean[targets.clamp(0, V - 1)], targets.clamp(max=-1))
+    w[masked, 0] = float("-inf")
+    wd = w.cuda()
+    loss, lse, rows = sk.entropy_fwd(h.cuda(), wd, targets.cuda(), "none")
+    check(h, w[keep], few, "none", None, loss, None, None)
+    up = torch.randn((T,), generator=torch.Generator().manual_seed(1), dtype=torch.float64).to(loss.dtype)
+    _, gw = sk.entropy_bwd(h.cuda(), wd, targets.cuda(), lse, rows, up.cuda(), "none", want_h=False)
+    assert torch.all(gw[masked.cuda()] == 0)
+    check(h, w[keep], few, "none", up, loss, None, gw[keep.cuda()])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_tiles_of_rows_that_end_within_a_step(dtype):
+    T, V, D = 2100, 5001, 200
+    h, w, targets = make(25, T, V, D, dtype)
+    check(h, w, targets, "mean", *run(h, w, targets))
