@@ -105,6 +105,35 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
         p.total = std::max<size_t>(at, 256);
     };
     const int64_t all = (V + kTileRows - 1) / kTileRows * kTileRows;
+    // Few classes of wide rows (1000 rows of 37449 floats, ten classes: loss 117 us by tiles and 42 like this, with gradients 448 and 231; narrow rows
+    // would leave most lanes of the gradients' kernel idle).  Ranges of 48 rows at least: their sums of grad_w are added up by one launch.
+    if (V <= 16 && D >= 512 && (backward || T > 16)) {
+        p.narrow = true;
+        p.piece = all;
+        p.pieces = 1;
+        const int64_t groups = std::max<int64_t>((T + 63) / 64, 1), each = 64 * 16 / p.size;   // of rows; columns that a wave takes at least
+        const int64_t cols = (D + each - 1) / each, blocks = (D * p.size + 4095) / 4096;
+        p.narrow_parts = (int)(parts ? std::max<int64_t>(1, std::min(1024 / groups, cols)) : 1);
+        p.narrow_columns = (cols + p.narrow_parts - 1) / p.narrow_parts * each;
+        p.narrow_parts = (int)((D + p.narrow_columns - 1) / p.narrow_columns);
+        p.narrow_ranges = (int)(parts ? std::max<int64_t>(1, std::min<int64_t>({1024 / blocks, (T + 47) / 48, ((int64_t)64 << 20) / (V * D * p.sum_size)})) : 1);
+        p.narrow_rows = std::max<int64_t>((T + p.narrow_ranges - 1) / p.narrow_ranges, 1);
+        size_t at = 0;
+        auto take = [&](int64_t entries, int size) {
+            const size_t here = at;
+            at += round_up((size_t)entries * size, 256);
+            return here;
+        };
+        p.off_z = take(p.narrow_parts * T * 16, p.sum_size);
+        p.off_max = p.off_up = take(T + 2, p.sum_size);
+        if (backward) {
+            p.off_g = take(T * 16, p.sum_size);
+            p.off_dw = take(p.narrow_ranges * V * D, p.sum_size);
+        }
+        p.total = std::max<size_t>(at, 256);
+        if (ws_bytes != 0 && p.total > ws_bytes && !least) return entropy_plan(backward, T, V, D, dt, true, 0);
+        return p;
+    }
     if (least) {   // the smallest pieces, or a single one: then grad_h needs no sums
         lay(all);
         const size_t single = p.total;

@@ -821,6 +821,7 @@ __global__ __launch_bounds__(256) void finish_kernel(const typename Types<T>::Su
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E; i < entries; i += (int64_t)gridDim.x * 256 * E) {
         const int n = entries - i < E ? (int)(entries - i) : E;
         Vec<S, E> x = n == E ? load_vec<S, E>(sum + i) : load_some<S, E>(sum + i, n);
+#pragma unroll 8
         for (int k = 1; k < parts; ++k) {
             const S* from = sum + k * entries + i;
             const Vec<S, E> y = n == E ? load_vec<S, E>(from) : load_some<S, E>(from, n);
@@ -833,6 +834,166 @@ __global__ __launch_bounds__(256) void finish_kernel(const typename Types<T>::Su
         if (n == E) store_vec(out + i, v);
         else store_some(out + i, v, n);
     }
+}
+
+// ------------------------------------------------------------------------------------------------ few classes
+// At most 16 classes and wide rows (features of signatures and a handful of labels): h is what is read, w fits in registers.  Tiles of 64 classes and
+// copies of h in whole steps would move h six times in a training step; here it is read for the loss, read again for the logits' gradients and read once
+// more while grad_h is written.
+constexpr int kFewClasses = 16;
+
+// z[part][row][16]: a wave takes 16 rows and a part of their columns, straight from memory.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void narrow_logits_kernel(const T* h, const T* w, int64_t rows, int classes, int64_t D, int64_t columns,
+                                                                 typename Types<T>::Sum* z)
+{
+    using Frag = typename Types<T>::Frag;
+    constexpr int E = kPer16<T>, U = 8;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t m0 = ((int64_t)blockIdx.x * 4 + wave) * 16, row = m0 + (lane & 15);
+    if (m0 >= rows) return;
+    const int64_t first = (int64_t)blockIdx.y * columns, end = first + columns < D ? first + columns : D;
+    const T* from_h = h + (row < rows ? row : rows - 1) * D + (lane >> 4) * E;
+    const T* from_w = w + (int64_t)((lane & 15) < classes ? lane & 15 : classes - 1) * D + (lane >> 4) * E;
+    typename Types<T>::Acc acc[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = {0, 0, 0, 0};
+    auto frag = [](const T* p) {
+        Frag f;
+        __builtin_memcpy(&f, p, 16);
+        return f;
+    };
+    int64_t k = first;
+    for (; k + U * 4 * E <= end; k += U * 4 * E) {
+        Frag a[U], b[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) a[u] = frag(from_h + k + u * 4 * E);
+#pragma unroll
+        for (int u = 0; u < U; ++u) b[u] = frag(from_w + k + u * 4 * E);
+#pragma unroll
+        for (int u = 0; u < U; ++u) acc[u % 4] = Types<T>::product(a[u], b[u], acc[u % 4]);
+    }
+    for (; k < end; k += 4 * E) {
+        const int64_t left = end - k - (lane >> 4) * E;
+        const int n = left >= E ? E : left > 0 ? (int)left : 0;
+        const Vec<T, E> va = load_some<T, E>(from_h + k, n), vb = load_some<T, E>(from_w + k, n);
+        Frag a, b;
+        __builtin_memcpy(&a, &va, 16);
+        __builtin_memcpy(&b, &vb, 16);
+        acc[0] = Types<T>::product(a, b, acc[0]);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int64_t at = m0 + acc_row<T>(lane, r);
+        if (at < rows) z[((int64_t)blockIdx.y * rows + at) * kFewClasses + (lane & 15)] = (acc[0][r] + acc[1][r]) + (acc[2][r] + acc[3][r]);
+    }
+}
+
+// 16 lanes per row add the parts.  Forward (g null): lse and the row's loss; backward: the logits' gradients g[row][16], not rounded.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void narrow_rows_kernel(const typename Types<T>::Sum* z, int parts, int64_t rows, int classes, const void* targets,
+                                                               int it, typename Types<T>::Sum* lse, typename Types<T>::Sum* losses,
+                                                               const typename Types<T>::Sum* up, typename Types<T>::Sum* g)
+{
+    using S = typename Types<T>::Sum;
+    const int lane = threadIdx.x & 15;
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
+    const bool there = row < rows;
+    const int64_t at = there ? row : rows - 1;
+    S x = 0;
+#pragma unroll 8
+    for (int k = 0; k < parts; ++k) x += z[((int64_t)k * rows + at) * kFewClasses + lane];
+    const int64_t target = load_index(targets, at, it);
+    if (g) {
+        const S u = up[at], p = exp_of(x - lse[at], T{}) - (target == lane ? (S)1 : (S)0);
+        if (there) g[row * kFewClasses + lane] = u != 0 && lane < classes ? u * p : (S)0;
+        return;
+    }
+    if (lane >= classes) x = lowest<S>();
+    S top = larger(x, lowest<S>());
+#pragma unroll
+    for (int o = 8; o > 0; o /= 2) top = larger(top, __shfl_xor(top, o));
+    S sum = exp_below<T>(x, top);
+#pragma unroll
+    for (int o = 8; o > 0; o /= 2) sum += __shfl_xor(sum, o);
+    const bool has = target >= 0 && target < classes;
+    const S hit = __shfl(x, has ? (int)target : 0, 16), l = top + log_of(sum);
+    if (there && lane == 0) {
+        lse[row] = l;
+        losses[row] = has ? l - hit : (S)0;
+    }
+}
+
+// grad_h[row] = g[row] w, and dw[part] = the sum over the part's rows of g[row]^T h[row]: a lane keeps E columns of w, and of the sums, for all classes.
+// Rows whose upstream is 0 are zeros and left out, whatever they hold.  E: 16 bytes, 8 of 16-bit types (32 registers of w and as many of sums
+// per two columns of double).  CLASSES: 4, 8 or 16, whichever holds them.
+template <typename T>
+constexpr int kNarrowCols = sizeof(T) == 8 ? 2 : 4;
+template <typename T, int CLASSES>
+__global__ __launch_bounds__(kThreads) void narrow_grads_kernel(const T* __restrict__ h, const T* __restrict__ w,
+                                                                const typename Types<T>::Sum* __restrict__ g,
+                                                                const typename Types<T>::Sum* __restrict__ up,
+                                                                const typename Types<T>::Sum* __restrict__ scaling, int64_t rows, int64_t rows_each, int classes,
+                                                                int64_t D, T* grad_h, typename Types<T>::Sum* dw)
+{
+    using S = typename Types<T>::Sum;
+    constexpr int E = kNarrowCols<T>, U = 8;
+    const int64_t col = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * E;
+    if (col >= D) return;
+    const int width = D - col < E ? (int)(D - col) : E;
+    const S f = *scaling;
+    S ws[CLASSES][E], sums[CLASSES][E];
+#pragma unroll
+    for (int v = 0; v < CLASSES; ++v) {
+        const Vec<T, E> x = v >= classes ? load_some<T, E>(w, 0) : width == E ? load_vec<T, E>(w + v * D + col) : load_some<T, E>(w + v * D + col, width);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            ws[v][e] = (S)x.v[e];
+            sums[v][e] = 0;
+        }
+    }
+    const int64_t first = (int64_t)blockIdx.y * rows_each, end = first + rows_each < rows ? first + rows_each : rows;
+    for (int64_t t = first; t < end; t += U) {
+        Vec<T, E> x[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const T* from = h + (t + i < end ? t + i : t) * D + col;
+            if (dw) x[i] = width == E ? load_vec<T, E>(from) : load_some<T, E>(from, width);
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (t + i >= end) break;
+            const S* gr = g + (t + i) * kFewClasses;
+            const bool some = up[t + i] != 0;
+            S y[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) y[e] = 0;
+            if (some)
+#pragma unroll
+                for (int v = 0; v < CLASSES; ++v) {
+                    const S q = gr[v];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        y[e] += q * ws[v][e];
+                        if (dw) sums[v][e] += q * (S)x[i].v[e];
+                    }
+                }
+            if (grad_h) {
+                Vec<T, E> out;
+#pragma unroll
+                for (int e = 0; e < E; ++e) out.v[e] = scaled<T>(y[e], f);
+                if (width == E) store_vec(grad_h + (t + i) * D + col, out);
+                else store_some(grad_h + (t + i) * D + col, out, width);
+            }
+        }
+    }
+    if (!dw) return;
+#pragma unroll
+    for (int v = 0; v < CLASSES; ++v)
+        if (v < classes)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e < width) dw[((int64_t)blockIdx.y * classes + v) * D + col + e] = sums[v][e];
 }
 
 // ------------------------------------------------------------------------------------------------ copies
@@ -1137,6 +1298,16 @@ hipError_t entropy_run_fwd(const EntropyPlan& p, const T* h, const T* w, const v
         return hipSuccess;
     }
     S *run_max = reinterpret_cast<S*>(ws + p.off_max), *run_sum = reinterpret_cast<S*>(ws + p.off_sum), *hit = reinterpret_cast<S*>(ws + p.off_hit);
+    if (p.narrow) {
+        S* z = reinterpret_cast<S*>(ws + p.off_z);
+        S* losses = reduction == ST_NONE ? static_cast<S*>(loss) : run_max;
+        ST_TRY((narrow_logits_kernel<T><<<dim3((unsigned)((p.T + 63) / 64), (unsigned)p.narrow_parts), kThreads, 0, st>>>(h, w, p.T, (int)p.V, p.D,
+                                                                                                                        p.narrow_columns, z)));
+        ST_TRY((narrow_rows_kernel<T><<<(unsigned)((p.T + 15) / 16), kThreads, 0, st>>>(z, p.narrow_parts, p.T, (int)p.V, targets, it, static_cast<S*>(lse),
+                                                                                       losses, nullptr, nullptr)));
+        ST_TRY((reduce_kernel<S><<<1, 1024, 0, st>>>(losses, targets, it, p.T, p.V, reduction, static_cast<S*>(loss), rows)));
+        return hipSuccess;
+    }
     const int64_t most = (p.piece + p.part_classes - 1) / p.part_classes;
     S *part_max = reinterpret_cast<S*>(ws + p.off_part), *part_sum = part_max + most * p.T;
     const T* hs = h;
@@ -1195,6 +1366,20 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
     T *ht = reinterpret_cast<T*>(ws + p.off_ht), *wt = reinterpret_cast<T*>(ws + p.off_wt);
     T *g = reinterpret_cast<T*>(ws + p.off_g), *gt = reinterpret_cast<T*>(ws + p.off_gt);
     ST_TRY((upstream_kernel<T><<<1, 1024, 0, st>>>(static_cast<const S*>(grad), targets, it, p.T, p.V, reduction, rows, up, scaling)));
+    if (p.narrow) {
+        S *z = reinterpret_cast<S*>(ws + p.off_z), *gs = reinterpret_cast<S*>(ws + p.off_g), *dw = reinterpret_cast<S*>(ws + p.off_dw);
+        ST_TRY((narrow_logits_kernel<T><<<dim3((unsigned)((p.T + 63) / 64), (unsigned)p.narrow_parts), kThreads, 0, st>>>(h, w, p.T, (int)p.V, p.D,
+                                                                                                                        p.narrow_columns, z)));
+        ST_TRY((narrow_rows_kernel<T><<<(unsigned)((p.T + 15) / 16), kThreads, 0, st>>>(z, p.narrow_parts, p.T, (int)p.V, targets, it,
+                                                                                       static_cast<S*>(const_cast<void*>(lse)), nullptr, up, gs)));
+        const int64_t per = kThreads * kNarrowCols<T>;
+        const auto grads = p.V <= 4 ? narrow_grads_kernel<T, 4> : p.V <= 8 ? narrow_grads_kernel<T, 8> : narrow_grads_kernel<T, kFewClasses>;
+        ST_TRY((grads<<<dim3((unsigned)((p.D + per - 1) / per), (unsigned)p.narrow_ranges), kThreads, 0, st>>>(
+            h, w, gs, up, scaling, p.T, p.narrow_rows, (int)p.V, p.D, grad_h, grad_w ? dw : nullptr)));
+        if (grad_w)
+            ST_TRY((finish_kernel<T><<<blocks_for((p.V * p.D + 3) / 4), 256, 0, st>>>(dw, p.narrow_ranges, p.V * p.D, scaling, grad_w)));
+        return hipSuccess;
+    }
     const T* hs;
     int64_t h_pitch = p.Dp;
     hipError_t e = in_steps(h, p.T, p.T, p.D, &h_pitch, ws + p.off_h, &hs, false, st);

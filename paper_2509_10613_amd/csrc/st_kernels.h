@@ -46,7 +46,10 @@ struct EntropyPlan {
     int64_t Dp, Tp;            // D and T in whole steps
     int64_t piece, pieces;     // classes per piece (a multiple of kTileRows)
     bool few;                  // forward, of at most 16 rows: w is read straight from memory
-    int64_t part_classes;      // ... classes whose maximum and sum are formed together
+    bool narrow;               // at most 16 classes and wide rows: h is read straight from memory
+    int narrow_parts, narrow_ranges;             // ... in parts of its columns for the logits, in ranges of its rows for grad_w
+    int64_t narrow_columns, narrow_rows;         // ... of so many
+    int64_t part_classes;      // forward: classes whose maximum and sum are formed together
     Tiling logits, by_h, by_w; // the products of the logits and of both gradients
     bool sums;                 // whether grad_h is summed over pieces or parts
     size_t off_h, off_w;       // copies of h and of a piece of w with rows of Dp (used where the caller's do not fit)

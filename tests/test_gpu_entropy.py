@@ -401,3 +401,29 @@ def test_large_tiles_of_rows_that_end_within_a_step(dtype):
     T, V, D = 2100, 5001, 200
     h, w, targets = make(25, T, V, D, dtype)
     check(h, w, targets, "mean", *run(h, w, targets))
+
+
+# at most 16 classes and wide rows: one class and all 16, columns of parts and of one, rows of one wave and of several ranges
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V,D", [(1, 3, 600), (17, 1, 512), (30, 2, 1001), (130, 10, 5461), (3000, 16, 515), (700, 7, 2048), (64, 16, 20000)])
+def test_few_classes_of_wide_rows(T, V, D, dtype):
+    h, w, targets = make(T + V + D, T, V, D, dtype, outside=0.2 if T > 1 else 0.0)
+    for reduction in ("mean", "none"):
+        check(h, w, targets, reduction, *run(h, w, targets, reduction))
+    clean = run(h, w, targets)
+    dirty = h.clone()
+    dirty[(targets < 0) | (targets >= V)] = float("nan")
+    assert all(torch.equal(a.cpu(), b.cpu()) for a, b in zip(clean, run(dirty, w, targets)))
+    hd, wd, td = h.cuda(), w.cuda(), targets.cuda()
+    size = sk.load().sigtrain_entropy_workspace_bytes
+    for least in (0, 1):   # a workspace of the least bytes, and nothing written behind it
+        sizes = [int(size(b, T, V, D, sk._ST_TYPES[dtype], least)) for b in (0, 1)]
+        bufs = [torch.full((n + 4096,), 77, dtype=torch.uint8, device="cuda") for n in sizes]
+        loss, lse, rows = sk.entropy_fwd(hd, wd, td, "sum", ws=bufs[0][:sizes[0]])
+        gh, gw = sk.entropy_bwd(hd, wd, td, lse, rows, torch.ones_like(loss), "sum", ws=bufs[1][:sizes[1]])
+        check(h, w, targets, "sum", torch.ones((), dtype=loss.dtype), loss, gh, gw)
+        assert all(torch.all(b[n:] == 77) for b, n in zip(bufs, sizes))
+        only_h = sk.entropy_bwd(hd, wd, td, lse, rows, torch.ones_like(loss), "sum", want_w=False)[0]
+        only_w = sk.entropy_bwd(hd, wd, td, lse, rows, torch.ones_like(loss), "sum", want_h=False)[1]
+        assert torch.equal(only_h, sk.entropy_bwd(hd, wd, td, lse, rows, torch.ones_like(loss), "sum")[0])
+        assert torch.equal(only_w, sk.entropy_bwd(hd, wd, td, lse, rows, torch.ones_like(loss), "sum")[1])
