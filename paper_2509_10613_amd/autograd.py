@@ -22,6 +22,9 @@ library's flag takes t_i = i/(L-1)) is an ordinary channel: ``with_times(x, t)``
 
 The gradients are first-order only (the backward pass is not itself differentiable).
 
+To capture a training step into a graph, take its gradients with ``torch.autograd.grad``, or let no eager graph of the same leaves live
+while ``backward()`` is captured: such a graph's accumulation nodes belong to another stream, which PyTorch then waits for inside the capture.
+
 A forward call on inputs that require gradients keeps what it sweeps for its backward call where the launch mode has such a
 form, and for few pairs also makes the adjoint sweep, beside its own.  It does so whether or not a backward call follows:
 evaluate under ``torch.no_grad()``.  Under saved-tensor hooks (checkpoints, ``save_on_cpu``) it keeps nothing.
