@@ -1,7 +1,7 @@
 // The norm of all entries of many arrays, and the arrays scaled down to a bound.
 //
 // Bound by memory: one read for the norm, one read and one write for the scaling (the factor is known only after the whole first
-// pass; what of the arrays the caches still hold is not read again).  The arrays' table travels as a kernel argument, so a call
+// pass; what of the arrays the caches still hold is not read again): 1.64e9 bfloat16 entries into floats 2.74 ms, 4.8 TB/s.  The arrays' table travels as a kernel argument, so a call
 // copies nothing and can be captured; kClipBatch arrays per launch.  A launch is one grid of workgroups that step through
 // chunks of kChunk entries, whatever arrays these lie in, and leaves one partial sum of squares per workgroup; every workgroup of the
 // scaling launches adds all partial sums in the same order, which is cheaper than a launch in between.
