@@ -237,8 +237,14 @@ int sigtrain_describe(int op, int64_t n, int64_t V, int64_t D, st_dtype dt, size
                  p.passes, p.bits, p.lanes, p.slices, (long long)p.units, (long long)p.groups, p.total);
     } else {
         const st::EntropyPlan p = st::entropy_plan(op == 3, n, V, D, dt, false, ws_bytes);
-        snprintf(out, out_bytes, "%s piece=%lld pieces=%lld ws=%zu", op == 3 ? "entropy_bwd" : "entropy_fwd", (long long)p.piece, (long long)p.pieces,
-                 p.total);
+        const int used = snprintf(out, out_bytes, "%s piece=%lld pieces=%lld ws=%zu", op == 3 ? "entropy_bwd" : "entropy_fwd", (long long)p.piece,
+                                  (long long)p.pieces, p.total);
+        if (op == 3 && !p.narrow && used > 0 && (size_t)used < out_bytes) {
+            const int64_t per = st::kStepBytes / p.size, last = V - (p.pieces - 1) * p.piece, whole = p.piece < V ? p.piece : V;
+            const int64_t steps = (whole + per - 1) / per, last_steps = (last + per - 1) / per;
+            snprintf(out + used, out_bytes - used, " grad_h_steps=%lld parts=%d last_steps=%lld last_parts=%d", (long long)steps,
+                     st::parts_of(p.by_h, steps), (long long)last_steps, st::parts_of(p.by_h, last_steps));
+        }
     }
     return SK_OK;
 }

@@ -743,7 +743,8 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void grads_kernel(Opera
 }
 
 // out[n][m] (pitch D) = the products times *unscale, rounded; or, with SUMS, sum[part][n][m] = the products over the part's steps, added to
-// what is there unless `first`.  parts: the steps are divided among this many workgroups per tile.
+// what is there unless `first`.  parts: the steps are divided among this many workgroups per tile, one step each at least (the main loop multiplies one
+// whatever it is told).  A call with fewer parts than the first adds to the first of the sums.
 template <typename T, int SUB, bool SUMS, bool TURN_A, bool TURN_B>
 __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Operands o, TileOrder order, typename Types<T>::Sum* sum, T* out, int64_t D, bool first,
                                                               const typename Types<T>::Sum* unscale)
@@ -1281,7 +1282,7 @@ hipError_t launch_sums(const Operands& o, Tiling t, typename Types<T>::Sum* sum,
 {
     return with_sub<T>(t.sub, [&](auto sub) {
         constexpr int SUB = decltype(sub)::value;
-        return launch_product<T, SUB>(product_kernel<T, SUB, true, TURN_A, TURN_B>, o, t.parts, st, sum, (T*)nullptr, pitch, first,
+        return launch_product<T, SUB>(product_kernel<T, SUB, true, TURN_A, TURN_B>, o, parts_of(t, o.steps), st, sum, (T*)nullptr, pitch, first,
                                       (const typename Types<T>::Sum*)nullptr);
     });
 }

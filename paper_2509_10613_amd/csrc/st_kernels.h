@@ -40,6 +40,8 @@ constexpr int kTileRows = 256;    // pieces of the classes are multiples of this
 struct Tiling {
     int sub = 2, parts = 1;       // 16 x 16 tiles on a side of a wave's, and workgroups that divide a tile's steps
 };
+// The workgroups that divide `steps`: each takes one step at least.  (Parts are chosen for a whole piece of the classes; the last may have fewer steps.)
+inline int parts_of(const Tiling& t, int64_t steps) { return steps < t.parts ? (int)steps : t.parts; }
 struct EntropyPlan {
     int64_t T, V, D;
     int size, sum_size;        // bytes of an element and of a sum
