@@ -49,14 +49,14 @@ enum { ST_NONE = 0, ST_MEAN = 1, ST_SUM = 2 };
 /*
  * Softmax cross entropy of the linear read-out z = h w^T, h[T, D], w[V, D]:
  *     lse[t] = log sum_v exp z[t, v],   row t's loss = lse[t] - z[t, targets[t]].
- * A row whose target is outside 0 .. V - 1 has no target (padding, a prompt): its loss is 0, its gradient is 0, it is not counted
- * and what its row of h holds reaches neither the loss nor grad_w.
+ * A row whose target is outside 0 .. V - 1 has no target (padding, a prompt): its loss is 0, its gradient is 0 (whatever the read-out
+ * holds), it is not counted and what its row of h holds reaches neither the loss nor grad_w.
  * reduction ST_NONE: loss[T]; ST_SUM: loss[1]; ST_MEAN: loss[1], the sum divided by the number of rows with a target (0 if there are none).
  * loss and lse are arrays of float (double for ST_F64); rows with a target, as a double: *rows.
  * Products are summed in float (double for ST_F64), and logits are never rounded to fewer bits.
  *
  * Backward: `grad` is dF/dloss, shaped and typed as `loss`; lse and rows are the forward call's.  grad_h[T, D] and grad_w[V, D]
- * (either may be NULL).  The logits' gradients u_t (exp(z - lse) - [v = target]) of a piece of the classes are rounded to the arrays' type before they
+ * (either may be NULL).  With ST_NONE a row whose upstream gradient is 0 is left out as one without a target.  The logits' gradients u_t (exp(z - lse) - [v = target]) of a piece of the classes are rounded to the arrays' type before they
  * are multiplied by w and h: divided by the largest |u_t| (the mean's and the sum's common factor, which 16-bit types need not hold), for ST_F16
  * times 2^14, so that small probabilities stay in its range; the products are multiplied by that again, in the sums' type.
  *

@@ -742,12 +742,13 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void grads_kernel(Opera
     }
 }
 
-// out[n][m] (pitch D) = the products times *unscale, rounded; or, with SUMS, sum[part][n][m] = the products over the part's steps, added to
+// out[n][m] (pitch D) = the products times *unscale, rounded, and 0 in the rows whose up[n] is 0 (of grad_h; null: none): 0 times an infinity of the
+// read-out is no gradient of a row that has no target; or, with SUMS, sum[part][n][m] = the products over the part's steps, added to
 // what is there unless `first`.  parts: the steps are divided among this many workgroups per tile, one step each at least (the main loop multiplies one
 // whatever it is told).  A call with fewer parts than the first adds to the first of the sums.
 template <typename T, int SUB, bool SUMS, bool TURN_A, bool TURN_B>
 __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Operands o, TileOrder order, typename Types<T>::Sum* sum, T* out, int64_t D, bool first,
-                                                              const typename Types<T>::Sum* unscale)
+                                                              const typename Types<T>::Sum* unscale, const typename Types<T>::Sum* up)
 {
     using S = typename Types<T>::Sum;
     using P = Product<T, SUB, TURN_A, TURN_B>;
@@ -774,6 +775,7 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Ope
     for (int j = 0; j < SUB; ++j) {
         const int64_t n = n0 + wn * kWave + j * 16 + (lane & 15);
         if (n >= o.n) continue;
+        const bool none = !SUMS && up && up[n] == 0;
 #pragma unroll
         for (int i = 0; i < SUB; ++i) {
             const int col = wm * kWave + i * 16 + acc_row<T>(lane, 0);
@@ -798,7 +800,7 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Ope
             } else {
                 Vec<T, 4> v;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v.v[r] = scaled<T>(x.v[r], f);
+                for (int r = 0; r < 4; ++r) v.v[r] = none ? T(0) : scaled<T>(x.v[r], f);
                 if constexpr (sizeof(T) == 2) outbox.put(wn * kWave + j * 16 + (lane & 15), col, v);
                 else if (kApart == 1 && m + 3 < o.m) store_vec(out + at, v);
                 else
@@ -811,10 +813,10 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Ope
     if constexpr (sizeof(T) == 2 && !SUMS) outbox.send(out + n0 * D + m0, D, o.n - n0, o.m - m0);
 }
 
-// out = the parts' sums in their order, times *unscale, rounded.
+// out = the parts' sums in their order, times *unscale, rounded; 0 in the rows, of D entries, whose `up` is 0 (null: none).
 template <typename T>
 __global__ __launch_bounds__(256) void finish_kernel(const typename Types<T>::Sum* sum, int parts, int64_t entries, const typename Types<T>::Sum* unscale,
-                                                     T* out)
+                                                     T* out, int64_t D, const typename Types<T>::Sum* up)
 {
     using S = typename Types<T>::Sum;
     constexpr int E = 16 / sizeof(S);
@@ -832,6 +834,17 @@ __global__ __launch_bounds__(256) void finish_kernel(const typename Types<T>::Su
         Vec<T, E> v;
 #pragma unroll
         for (int e = 0; e < E; ++e) v.v[e] = scaled<T>(x.v[e], f);
+        if (up) {
+            int64_t row = i / D, left = D - (i - row * D);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if (e < n && up[row] == 0) v.v[e] = T(0);
+                if (--left == 0) {
+                    ++row;
+                    left = D;
+                }
+            }
+        }
         if (n == E) store_vec(out + i, v);
         else store_some(out + i, v, n);
     }
@@ -926,7 +939,7 @@ __global__ __launch_bounds__(kThreads) void narrow_rows_kernel(const typename Ty
 }
 
 // grad_h[row] = g[row] w, and dw[part] = the sum over the part's rows of g[row]^T h[row]: a lane keeps E columns of w, and of the sums, for all classes.
-// Rows whose upstream is 0 are zeros and left out, whatever they hold.  E: 16 bytes, 8 of 16-bit types (32 registers of w and as many of sums
+// Rows whose upstream is 0 are zeros and left out, whatever they and the read-out hold.  E: 16 bytes, 8 of 16-bit types (32 registers of w and as many of sums
 // per two columns of double).  CLASSES: 4, 8 or 16, whichever holds them.
 template <typename T>
 constexpr int kNarrowCols = sizeof(T) == 8 ? 2 : 4;
@@ -998,20 +1011,17 @@ __global__ __launch_bounds__(kThreads) void narrow_grads_kernel(const T* __restr
 }
 
 // ------------------------------------------------------------------------------------------------ copies
-// dst[all][pitch] = src[rows][cols], zeros behind the columns and the rows.  targets not null: rows without one are zeros, whatever they hold.
+// dst[all][pitch] = src[rows][cols], zeros behind the columns and the rows.  up not null: rows whose `up` is 0 are zeros, whatever they hold.
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(const T* src, T* dst, int64_t rows, int64_t all, int64_t cols, int64_t pitch, const void* targets,
-                                                   int it, int64_t V)
+__global__ __launch_bounds__(256) void pack_kernel(const T* src, T* dst, int64_t rows, int64_t all, int64_t cols, int64_t pitch,
+                                                   const typename Types<T>::Sum* up)
 {
     constexpr int E = kPer16<T>;
     const int64_t per_row = pitch / E, items = all * per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / per_row, col = (i - row * per_row) * E;
         int64_t left = row < rows ? cols - col : 0;
-        if (targets && row < rows) {
-            const int64_t t = load_index(targets, row, it);
-            if (t < 0 || t >= V) left = 0;
-        }
+        if (up && row < rows && up[row] == 0) left = 0;
         const T* from = src + row * cols + col;
         store_vec(dst + row * pitch + col, left >= E ? load_vec<T, E>(from) : load_some<T, E>(from, (int)(left > 0 ? left : 0)));
     }
@@ -1023,13 +1033,13 @@ __global__ __launch_bounds__(256) void zero_kernel(T* p, int64_t n)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = T(0);
 }
 
-// dst[cols][pitch] = src[rows][cols] transposed, zeros behind the rows.  targets not null: rows without one are zeros, whatever they hold.
+// dst[cols][pitch] = src[rows][cols] transposed, zeros behind the rows.  up not null: rows whose `up` is 0 are zeros, whatever they hold.
 // A workgroup turns 64 x 64 entries (32 x 64 of double), moved as 16 bytes either way.
 template <typename T>
 constexpr int kTurnCols = sizeof(T) == 8 ? 32 : 64;
 template <typename T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* src, T* dst, int64_t rows, int64_t cols, int64_t pitch, const void* targets,
-                                                        int it, int64_t V)
+__global__ __launch_bounds__(256) void transpose_kernel(const T* src, T* dst, int64_t rows, int64_t cols, int64_t pitch,
+                                                        const typename Types<T>::Sum* up)
 {
     constexpr int R = 64, C = kTurnCols<T>, E = kPer16<T>, kPad = 4 / sizeof(T) ? 4 / sizeof(T) : 1;
     __shared__ T tile[C][R + kPad];   // (an odd number of words from column to column, or of double words)
@@ -1037,11 +1047,7 @@ __global__ __launch_bounds__(256) void transpose_kernel(const T* src, T* dst, in
     for (int i = threadIdx.x; i < R * C / E; i += 256) {
         const int row = i / (C / E), col = i % (C / E) * E;
         const int64_t r = r0 + row, left = cols - c0 - col;
-        bool there = r < rows && left > 0;
-        if (there && targets) {
-            const int64_t t = load_index(targets, r, it);
-            there = t >= 0 && t < V;
-        }
+        const bool there = r < rows && left > 0 && !(up && up[r] == 0);
         Vec<T, E> v;
         const T* from = src + r * cols + c0 + col;
         if (there && left >= E) v = load_vec<T, E>(from);
@@ -1233,7 +1239,7 @@ hipError_t in_steps(const T* src, int64_t rows, int64_t all, int64_t cols, int64
         return hipSuccess;
     }
     *out = static_cast<const T*>(copy);
-    ST_TRY((pack_kernel<T><<<blocks_for(all * (*pitch / kPer16<T>)), 256, 0, st>>>(src, static_cast<T*>(copy), rows, all, cols, *pitch, nullptr, 0, 0)));
+    ST_TRY((pack_kernel<T><<<blocks_for(all * (*pitch / kPer16<T>)), 256, 0, st>>>(src, static_cast<T*>(copy), rows, all, cols, *pitch, nullptr)));
     return hipSuccess;
 }
 // The logits' operands: classes of w, in rows of `pitch`, and h in whole steps (whose first row, where D is none, has zeros behind it).
@@ -1283,7 +1289,7 @@ hipError_t launch_sums(const Operands& o, Tiling t, typename Types<T>::Sum* sum,
     return with_sub<T>(t.sub, [&](auto sub) {
         constexpr int SUB = decltype(sub)::value;
         return launch_product<T, SUB>(product_kernel<T, SUB, true, TURN_A, TURN_B>, o, parts_of(t, o.steps), st, sum, (T*)nullptr, pitch, first,
-                                      (const typename Types<T>::Sum*)nullptr);
+                                      (const typename Types<T>::Sum*)nullptr, (const typename Types<T>::Sum*)nullptr);
     });
 }
 
@@ -1378,21 +1384,22 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
         ST_TRY((grads<<<dim3((unsigned)((p.D + per - 1) / per), (unsigned)p.narrow_ranges), kThreads, 0, st>>>(
             h, w, gs, up, scaling, p.T, p.narrow_rows, (int)p.V, p.D, grad_h, grad_w ? dw : nullptr)));
         if (grad_w)
-            ST_TRY((finish_kernel<T><<<blocks_for((p.V * p.D + 3) / 4), 256, 0, st>>>(dw, p.narrow_ranges, p.V * p.D, scaling, grad_w)));
+            ST_TRY((finish_kernel<T><<<blocks_for((p.V * p.D + 3) / 4), 256, 0, st>>>(dw, p.narrow_ranges, p.V * p.D, scaling, grad_w, p.D,
+                                                                                     nullptr)));
         return hipSuccess;
     }
     const T* hs;
     int64_t h_pitch = p.Dp;
     hipError_t e = in_steps(h, p.T, p.T, p.D, &h_pitch, ws + p.off_h, &hs, false, st);
     if (e != hipSuccess) return e;
-    auto turn = [&](const T* src, T* dst, int64_t r, int64_t pitch, const void* only) -> hipError_t {
+    auto turn = [&](const T* src, T* dst, int64_t r, int64_t pitch, const S* only) -> hipError_t {
         const dim3 grid((unsigned)((pitch + 63) / 64), (unsigned)((p.D + kTurnCols<T> - 1) / kTurnCols<T>));
-        ST_TRY((transpose_kernel<T><<<grid, 256, 0, st>>>(src, dst, r, p.D, pitch, only, it, p.V)));
+        ST_TRY((transpose_kernel<T><<<grid, 256, 0, st>>>(src, dst, r, p.D, pitch, only)));
         return hipSuccess;
     };
-    if (grad_w && !kTurned && (e = turn(h, ht, p.T, p.Tp, targets)) != hipSuccess) return e;
+    if (grad_w && !kTurned && (e = turn(h, ht, p.T, p.Tp, up)) != hipSuccess) return e;
     if (grad_w && kTurned)
-        ST_TRY((pack_kernel<T><<<blocks_for(p.Tp * (p.Dp / kPer16<T>)), 256, 0, st>>>(h, ht, p.T, p.Tp, p.D, p.Dp, targets, it, p.V)));
+        ST_TRY((pack_kernel<T><<<blocks_for(p.Tp * (p.Dp / kPer16<T>)), 256, 0, st>>>(h, ht, p.T, p.Tp, p.D, p.Dp, up)));
     for (int64_t i = 0; i < p.pieces; ++i) {
         const int64_t first = i * p.piece, n = p.V - first < p.piece ? p.V - first : p.piece;
         const int64_t per = kStepBytes / (int64_t)sizeof(T), np = (n + per - 1) / per * per;
@@ -1420,8 +1427,7 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
                 if (wsrc == w + first * p.D && n != np) {   // (behind the caller's last row nothing may be read)
                     o.a_tail = reinterpret_cast<const char*>(wt);
                     const int64_t whole = np - per;
-                    ST_TRY((pack_kernel<T><<<blocks_for(per * (pitch / kPer16<T>)), 256, 0, st>>>(wsrc + whole * pitch, wt, n - whole, per, p.D, pitch, nullptr,
-                                                                                                0, 0)));
+                    ST_TRY((pack_kernel<T><<<blocks_for(per * (pitch / kPer16<T>)), 256, 0, st>>>(wsrc + whole * pitch, wt, n - whole, per, p.D, pitch, nullptr)));
                 }
             } else {
                 if ((e = turn(w + first * p.D, wt, n, np, nullptr)) != hipSuccess) return e;
@@ -1431,7 +1437,8 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
             else
                 e = with_sub<T>(p.by_h.sub, [&](auto sub) {
                     constexpr int SUB = decltype(sub)::value;
-                    return launch_product<T, SUB>(product_kernel<T, SUB, false, kTurned, false>, o, 1, st, (S*)nullptr, grad_h, p.D, true, (const S*)scaling);
+                    return launch_product<T, SUB>(product_kernel<T, SUB, false, kTurned, false>, o, 1, st, (S*)nullptr, grad_h, p.D, true, (const S*)scaling,
+                                                   (const S*)up);
                 });
             if (e != hipSuccess) return e;
         }
@@ -1440,19 +1447,20 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
             if (p.by_w.parts > 1) {
                 S* dw = reinterpret_cast<S*>(ws + p.off_dw);
                 if ((e = launch_sums<T, kTurned, kTurned>(o, p.by_w, dw, p.D, true, st)) != hipSuccess) return e;
-                ST_TRY((finish_kernel<T><<<blocks_for((n * p.D + 3) / 4), 256, 0, st>>>(dw, p.by_w.parts, n * p.D, scaling, grad_w + first * p.D)));
+                ST_TRY((finish_kernel<T><<<blocks_for((n * p.D + 3) / 4), 256, 0, st>>>(dw, p.by_w.parts, n * p.D, scaling, grad_w + first * p.D, p.D,
+                                                                                            nullptr)));
                 continue;
             }
             e = with_sub<T>(p.by_w.sub, [&](auto sub) {
                 constexpr int SUB = decltype(sub)::value;
                 return launch_product<T, SUB>(product_kernel<T, SUB, false, kTurned, kTurned>, o, 1, st, (S*)nullptr, grad_w + first * p.D, p.D, true,
-                                              (const S*)scaling);
+                                              (const S*)scaling, (const S*)nullptr);
             });
             if (e != hipSuccess) return e;
         }
     }
     if (grad_h && p.sums)
-        ST_TRY((finish_kernel<T><<<blocks_for((p.T * p.D + 3) / 4), 256, 0, st>>>(dh, p.by_h.parts, p.T * p.D, scaling, grad_h)));
+        ST_TRY((finish_kernel<T><<<blocks_for((p.T * p.D + 3) / 4), 256, 0, st>>>(dh, p.by_h.parts, p.T * p.D, scaling, grad_h, p.D, up)));
     return hipSuccess;
 }
 
