@@ -56,9 +56,11 @@ enum { ST_NONE = 0, ST_MEAN = 1, ST_SUM = 2 };
  * Products are summed in float (double for ST_F64), and logits are never rounded to fewer bits.
  *
  * Backward: `grad` is dF/dloss, shaped and typed as `loss`; lse and rows are the forward call's.  grad_h[T, D] and grad_w[V, D]
- * (either may be NULL).  With ST_NONE a row whose upstream gradient is 0 is left out as one without a target.  The logits' gradients u_t (exp(z - lse) - [v = target]) of a piece of the classes are rounded to the arrays' type before they
- * are multiplied by w and h: divided by the largest |u_t| (the mean's and the sum's common factor, which 16-bit types need not hold), for ST_F16
- * times 2^14, so that small probabilities stay in its range; the products are multiplied by that again, in the sums' type.
+ * (either may be NULL).  With ST_NONE a row whose upstream gradient is 0 is left out as one without a target.  The logits' gradients
+ * u_t (exp(z - lse) - [v = target]) of a piece of the classes are rounded to the arrays' type before they are multiplied by w and h (except of at
+ * most 16 classes of wide rows): without the mean's and the sum's common factor, or, with ST_NONE, divided by the largest finite |u_t| and by the
+ * power of two that this leaves of their own row, none of which 16-bit types need hold; for ST_F16 times 2^14, so that small probabilities stay in its range.  The
+ * products are multiplied by all of that again, in the sums' type; the rows of h that grad_w is made from have the powers of two beforehand.
  *
  * The workspace query gives what the call is fastest with; with `least` set, what it takes (smaller pieces).
  */

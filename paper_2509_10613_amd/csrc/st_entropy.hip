@@ -94,6 +94,7 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
             p.by_w = choose_tiling(p.size, D, classes, p.Tp / per, parts && classes * D <= 1 << 24 ? 16 : 1, p.sum_size);
             p.sums = p.pieces > 1 || p.by_h.parts > 1;
             p.off_up = take(T + 2, p.sum_size);
+            p.off_exps = take(T + 1, 4);
             const bool turned = p.size == 2;   // (the products turn what others need turned copies of)
             p.off_ht = take(turned ? p.Tp * p.Dp : D * p.Tp, p.size);
             p.off_wt = take(turned ? per * p.Dp : D * piece, p.size);

@@ -14,6 +14,7 @@
 // grad_w: G and h) 16-bit operands are turned by the reads of LDS, others come from turned copies.
 #pragma once
 #include <algorithm>
+#include <climits>
 #include <utility>
 
 #include "st_dev.h"
@@ -450,11 +451,41 @@ struct Outbox {
     }
 };
 
-// A result in the arrays' type; a 0 stays one whatever is upstream (rows without a target).
-template <typename T, typename S>
-__device__ __forceinline__ T scaled(S x, S f)
+__device__ __forceinline__ float power(float x, int e) { return ldexpf(x, e); }   // x 2^e
+__device__ __forceinline__ double power(double x, int e) { return ldexp(x, e); }
+
+// What is upstream of the rows, as upstream_kernel divides it between the logits' gradients and the other sides of the products.  up: the part in the
+// logits' gradients (0: the row is left out).  exps (null: all 0): grad_h's row is 2^exps[t] times its products and *unscale, and the
+// row of h that grad_w is made from is 2^(exps[t] + shift) h[t].  largest: of that row's entries' exponents, before the shift, which puts it at 2^15;
+// w_unscale: what grad_w's products are multiplied by, written by the kernel that makes the copy of h.
+template <typename S>
+struct Upstream {
+    S* up = nullptr;
+    int* exps = nullptr;
+    int* largest = nullptr;
+    S *unscale = nullptr, *w_unscale = nullptr;
+
+    __device__ __forceinline__ int shift() const
+    {
+        const int top = *largest;
+        return top == INT_MIN ? 0 : 15 - top;   // (no entry counts: any does)
+    }
+    // (one thread of the launch that makes the copy)
+    __device__ __forceinline__ void put_w_unscale() const { *w_unscale = power(*unscale, -shift()); }
+    __device__ __forceinline__ int exponent(int64_t row) const { return exps ? exps[row] : 0; }
+};
+template <typename T, int E, typename S>
+__device__ __forceinline__ void times_power(Vec<T, E>& v, S, int e)
 {
-    return (T)(x == 0 ? x : x * f);
+#pragma unroll
+    for (int i = 0; i < E; ++i) v.v[i] = (T)power((S)v.v[i], e);
+}
+
+// A result in the arrays' type, f 2^e x; a 0 stays one whatever is upstream (rows without a target).
+template <typename T, typename S>
+__device__ __forceinline__ T scaled(S x, S f, int e)
+{
+    return (T)(x == 0 ? x : power(x * f, e));
 }
 struct NoOutbox {
     char* lds;
@@ -742,13 +773,13 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void grads_kernel(Opera
     }
 }
 
-// out[n][m] (pitch D) = the products times *unscale, rounded, and 0 in the rows whose up[n] is 0 (of grad_h; null: none): 0 times an infinity of the
-// read-out is no gradient of a row that has no target; or, with SUMS, sum[part][n][m] = the products over the part's steps, added to
+// out[n][m] (pitch D) = the products times *unscale and, of grad_h (`rows`), the rows' powers of two, rounded; 0 in the rows whose up[n] is 0: 0 times
+// an infinity of the read-out is no gradient of a row that has no target; or, with SUMS, sum[part][n][m] = the products over the part's steps, added to
 // what is there unless `first`.  parts: the steps are divided among this many workgroups per tile, one step each at least (the main loop multiplies one
 // whatever it is told).  A call with fewer parts than the first adds to the first of the sums.
 template <typename T, int SUB, bool SUMS, bool TURN_A, bool TURN_B>
 __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Operands o, TileOrder order, typename Types<T>::Sum* sum, T* out, int64_t D, bool first,
-                                                              const typename Types<T>::Sum* unscale, const typename Types<T>::Sum* up)
+                                                              const typename Types<T>::Sum* unscale, Upstream<typename Types<T>::Sum> rows)
 {
     using S = typename Types<T>::Sum;
     using P = Product<T, SUB, TURN_A, TURN_B>;
@@ -775,7 +806,8 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Ope
     for (int j = 0; j < SUB; ++j) {
         const int64_t n = n0 + wn * kWave + j * 16 + (lane & 15);
         if (n >= o.n) continue;
-        const bool none = !SUMS && up && up[n] == 0;
+        const bool none = !SUMS && rows.up && rows.up[n] == 0;
+        const int e = SUMS ? 0 : rows.exponent(n);
 #pragma unroll
         for (int i = 0; i < SUB; ++i) {
             const int col = wm * kWave + i * 16 + acc_row<T>(lane, 0);
@@ -800,7 +832,7 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Ope
             } else {
                 Vec<T, 4> v;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v.v[r] = none ? T(0) : scaled<T>(x.v[r], f);
+                for (int r = 0; r < 4; ++r) v.v[r] = none ? T(0) : scaled<T>(x.v[r], f, e);
                 if constexpr (sizeof(T) == 2) outbox.put(wn * kWave + j * 16 + (lane & 15), col, v);
                 else if (kApart == 1 && m + 3 < o.m) store_vec(out + at, v);
                 else
@@ -813,10 +845,10 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Ope
     if constexpr (sizeof(T) == 2 && !SUMS) outbox.send(out + n0 * D + m0, D, o.n - n0, o.m - m0);
 }
 
-// out = the parts' sums in their order, times *unscale, rounded; 0 in the rows, of D entries, whose `up` is 0 (null: none).
+// out = the parts' sums in their order, times *unscale and, of grad_h, the powers of two of its rows of D entries, rounded; 0 in the rows whose up is 0.
 template <typename T>
 __global__ __launch_bounds__(256) void finish_kernel(const typename Types<T>::Sum* sum, int parts, int64_t entries, const typename Types<T>::Sum* unscale,
-                                                     T* out, int64_t D, const typename Types<T>::Sum* up)
+                                                     T* out, int64_t D, Upstream<typename Types<T>::Sum> rows)
 {
     using S = typename Types<T>::Sum;
     constexpr int E = 16 / sizeof(S);
@@ -833,12 +865,12 @@ __global__ __launch_bounds__(256) void finish_kernel(const typename Types<T>::Su
         }
         Vec<T, E> v;
 #pragma unroll
-        for (int e = 0; e < E; ++e) v.v[e] = scaled<T>(x.v[e], f);
-        if (up) {
+        for (int e = 0; e < E; ++e) v.v[e] = scaled<T>(x.v[e], f, 0);
+        if (rows.up) {
             int64_t row = i / D, left = D - (i - row * D);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                if (e < n && up[row] == 0) v.v[e] = T(0);
+                if (e < n) v.v[e] = rows.up[row] == 0 ? T(0) : scaled<T>(x.v[e], f, rows.exponent(row));
                 if (--left == 0) {
                     ++row;
                     left = D;
@@ -995,7 +1027,7 @@ __global__ __launch_bounds__(kThreads) void narrow_grads_kernel(const T* __restr
             if (grad_h) {
                 Vec<T, E> out;
 #pragma unroll
-                for (int e = 0; e < E; ++e) out.v[e] = scaled<T>(y[e], f);
+                for (int e = 0; e < E; ++e) out.v[e] = scaled<T>(y[e], f, 0);
                 if (width == E) store_vec(grad_h + (t + i) * D + col, out);
                 else store_some(grad_h + (t + i) * D + col, out, width);
             }
@@ -1011,19 +1043,25 @@ __global__ __launch_bounds__(kThreads) void narrow_grads_kernel(const T* __restr
 }
 
 // ------------------------------------------------------------------------------------------------ copies
-// dst[all][pitch] = src[rows][cols], zeros behind the columns and the rows.  up not null: rows whose `up` is 0 are zeros, whatever they hold.
+// dst[all][pitch] = src[rows][cols], zeros behind the columns and the rows.  With `u` rows whose up is 0 are zeros, whatever they hold, and others
+// have their power of two.
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const T* src, T* dst, int64_t rows, int64_t all, int64_t cols, int64_t pitch,
-                                                   const typename Types<T>::Sum* up)
+                                                   Upstream<typename Types<T>::Sum> u)
 {
+    using S = typename Types<T>::Sum;
     constexpr int E = kPer16<T>;
+    if (u.exps && blockIdx.x == 0 && threadIdx.x == 0) u.put_w_unscale();
+    const int shift = u.exps ? u.shift() : 0;
     const int64_t per_row = pitch / E, items = all * per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / per_row, col = (i - row * per_row) * E;
         int64_t left = row < rows ? cols - col : 0;
-        if (up && row < rows && up[row] == 0) left = 0;
+        if (u.up && row < rows && u.up[row] == 0) left = 0;
         const T* from = src + row * cols + col;
-        store_vec(dst + row * pitch + col, left >= E ? load_vec<T, E>(from) : load_some<T, E>(from, (int)(left > 0 ? left : 0)));
+        Vec<T, E> v = left >= E ? load_vec<T, E>(from) : load_some<T, E>(from, (int)(left > 0 ? left : 0));
+        if (u.exps && left > 0) times_power(v, S{}, u.exps[row] + shift);
+        store_vec(dst + row * pitch + col, v);
     }
 }
 
@@ -1033,25 +1071,29 @@ __global__ __launch_bounds__(256) void zero_kernel(T* p, int64_t n)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = T(0);
 }
 
-// dst[cols][pitch] = src[rows][cols] transposed, zeros behind the rows.  up not null: rows whose `up` is 0 are zeros, whatever they hold.
+// dst[cols][pitch] = src[rows][cols] transposed, zeros behind the rows.  `u`: as in pack_kernel.
 // A workgroup turns 64 x 64 entries (32 x 64 of double), moved as 16 bytes either way.
 template <typename T>
 constexpr int kTurnCols = sizeof(T) == 8 ? 32 : 64;
 template <typename T>
 __global__ __launch_bounds__(256) void transpose_kernel(const T* src, T* dst, int64_t rows, int64_t cols, int64_t pitch,
-                                                        const typename Types<T>::Sum* up)
+                                                        Upstream<typename Types<T>::Sum> u)
 {
+    using S = typename Types<T>::Sum;
+    if (u.exps && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) u.put_w_unscale();
+    const int shift = u.exps ? u.shift() : 0;
     constexpr int R = 64, C = kTurnCols<T>, E = kPer16<T>, kPad = 4 / sizeof(T) ? 4 / sizeof(T) : 1;
     __shared__ T tile[C][R + kPad];   // (an odd number of words from column to column, or of double words)
     const int64_t r0 = (int64_t)blockIdx.x * R, c0 = (int64_t)blockIdx.y * C;
     for (int i = threadIdx.x; i < R * C / E; i += 256) {
         const int row = i / (C / E), col = i % (C / E) * E;
         const int64_t r = r0 + row, left = cols - c0 - col;
-        const bool there = r < rows && left > 0 && !(up && up[r] == 0);
+        const bool there = r < rows && left > 0 && !(u.up && u.up[r] == 0);
         Vec<T, E> v;
         const T* from = src + r * cols + c0 + col;
         if (there && left >= E) v = load_vec<T, E>(from);
         else v = load_some<T, E>(from, there ? (int)left : 0);
+        if (u.exps && there) times_power(v, S{}, u.exps[r] + shift);
 #pragma unroll
         for (int e = 0; e < E; ++e) tile[col + e][row] = v.v[e];
     }
@@ -1180,43 +1222,87 @@ __global__ __launch_bounds__(1024) void reduce_kernel(const S* losses, const voi
     if (reduction == ST_MEAN) *loss = (S)(n > 0 ? sum / n : 0.0);
 }
 
-// Every row's upstream gradient over the largest of them, and that one: scaling[0].  The logits' gradients are rounded to T, and a common
-// factor that T does not hold (one over the number of rows) would put all of them off by the same part of a step.  f16 takes 2^14 times as
-// much, or small probabilities would be subnormal.  One workgroup.
+// What is upstream of every row, divided (Upstream).  The logits' gradients are rounded to T, and a common factor that T does not hold (one over the
+// number of rows) would put all of them off by the same part of a step: it stays out of them.  Rows with upstream gradients of their own are divided by
+// the largest of them, and of what is left the powers of two stay out as well: float16 holds little more than the probabilities' range, and a
+// row's gradient of h is rounded as well as any other's however small the row's upstream is beside the largest.  f16 takes 2^14 times as much, or
+// small probabilities would be subnormal.  exps null (few classes: their logits' gradients are not rounded): nothing is divided.  One workgroup.
 template <typename T>
 __global__ __launch_bounds__(1024) void upstream_kernel(const typename Types<T>::Sum* grad, const void* targets, int it, int64_t rows, int64_t V,
-                                                        int reduction, const double* count, typename Types<T>::Sum* up,
-                                                        typename Types<T>::Sum* scaling)
+                                                        int reduction, const double* count, Upstream<typename Types<T>::Sum> u)
 {
     using S = typename Types<T>::Sum;
-    constexpr S kRange = std::is_same_v<T, f16> ? (S)16384 : (S)1;
+    constexpr int kRange = std::is_same_v<T, f16> ? 14 : 0;
     __shared__ S tops[16];
     auto has = [&](int64_t i) {
         const int64_t t = load_index(targets, i, it);
         return t >= 0 && t < V;
     };
-    S top = 1;
-    if (reduction == ST_NONE) {
-        top = 0;
-        for (int64_t i = threadIdx.x; i < rows; i += 1024) {
-            const S a = has(i) ? (grad[i] < 0 ? -grad[i] : grad[i]) : (S)0;
-            top = a > top ? a : top;
-        }
+    const S inf = (S)__builtin_inf();
+    if (reduction != ST_NONE || !u.exps) {
+        const S one = u.exps ? power((S)1, kRange) : (S)1;
+        for (int64_t i = threadIdx.x; i < rows; i += 1024) u.up[i] = !has(i) ? (S)0 : reduction == ST_NONE ? grad[i] : one;
+        if (threadIdx.x == 0)
+            *u.unscale = *u.w_unscale = (reduction == ST_MEAN ? (S)((double)grad[0] / *count) : reduction == ST_SUM ? grad[0] : (S)1) / one;
+        return;
+    }
+    S top = 0;
+    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
+        const S a = has(i) ? (grad[i] < 0 ? -grad[i] : grad[i]) : (S)0;
+        top = a > top && a < inf ? a : top;
+    }
 #pragma unroll
-        for (int o = 32; o > 0; o /= 2) {
-            const S a = __shfl_xor(top, o);
-            top = a > top ? a : top;
-        }
-        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-        __syncthreads();
-        for (int i = 0; i < 16; ++i) top = tops[i] > top ? tops[i] : top;
-        if (!(top > 0 && top < (S)__builtin_inf())) top = 1;
+    for (int o = 32; o > 0; o /= 2) {
+        const S a = __shfl_xor(top, o);
+        top = a > top ? a : top;
     }
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) up[i] = !has(i) ? (S)0 : reduction == ST_NONE ? grad[i] / top * kRange : kRange;
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int i = 0; i < 16; ++i) top = tops[i] > top ? tops[i] : top;
+    if (top == 0) top = 1;
+    int top_exp;
+    const S part = frexp(top, &top_exp);
+    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
+        const S x = has(i) ? grad[i] : (S)0;
+        int e = top_exp;
+        S y = x;   // 0, infinite or NaN
+        if (x != 0 && x > -inf && x < inf) y = frexp(x, &e) / part;
+        u.up[i] = power(y, kRange);
+        u.exps[i] = e - kRange;
+    }
     if (threadIdx.x == 0) {
-        const S all = reduction == ST_MEAN ? (S)((double)grad[0] / *count) : reduction == ST_SUM ? grad[0] : top;
-        *scaling = all / kRange;
+        *u.unscale = part;
+        *u.largest = kRange != 0 ? INT_MIN : 15 + top_exp;   // (a shift that takes the largest power of two away, or largest_kernel's)
     }
+}
+
+// The largest exponent among the entries of h, each with its row's power of two.  A wave per row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void largest_kernel(const T* h, int64_t rows, int64_t D, Upstream<typename Types<T>::Sum> u)
+{
+    using S = typename Types<T>::Sum;
+    constexpr int E = kPer16<T>;
+    const int lane = threadIdx.x & 63;
+    int largest = INT_MIN;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * 4) {
+        const S up = u.up[row];
+        if (up == 0 || !(up - up == 0)) continue;   // left out, or infinite
+        S top = 0;
+        for (int64_t k = lane * E; k < D; k += 64 * E) {
+            const Vec<T, E> v = D - k >= E ? load_vec<T, E>(h + row * D + k) : load_some<T, E>(h + row * D + k, (int)(D - k));
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const S a = (S)v.v[i] < 0 ? -(S)v.v[i] : (S)v.v[i];
+                top = a > top && a < (S)__builtin_inf() ? a : top;
+            }
+        }
+        int e;
+        frexp(top, &e);
+        if (top > 0) largest = max(largest, e + u.exps[row]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) largest = max(largest, __shfl_xor(largest, o));
+    if (lane == 0 && largest != INT_MIN) atomicMax(u.largest, largest);   // (a whole number: in any order)
 }
 
 unsigned blocks_for(int64_t items) { return (unsigned)((items + 255) / 256 < 16384 ? (items + 255) / 256 : 16384); }
@@ -1239,7 +1325,7 @@ hipError_t in_steps(const T* src, int64_t rows, int64_t all, int64_t cols, int64
         return hipSuccess;
     }
     *out = static_cast<const T*>(copy);
-    ST_TRY((pack_kernel<T><<<blocks_for(all * (*pitch / kPer16<T>)), 256, 0, st>>>(src, static_cast<T*>(copy), rows, all, cols, *pitch, nullptr)));
+    ST_TRY((pack_kernel<T><<<blocks_for(all * (*pitch / kPer16<T>)), 256, 0, st>>>(src, static_cast<T*>(copy), rows, all, cols, *pitch, Upstream<typename Types<T>::Sum>{})));
     return hipSuccess;
 }
 // The logits' operands: classes of w, in rows of `pitch`, and h in whole steps (whose first row, where D is none, has zeros behind it).
@@ -1289,7 +1375,7 @@ hipError_t launch_sums(const Operands& o, Tiling t, typename Types<T>::Sum* sum,
     return with_sub<T>(t.sub, [&](auto sub) {
         constexpr int SUB = decltype(sub)::value;
         return launch_product<T, SUB>(product_kernel<T, SUB, true, TURN_A, TURN_B>, o, parts_of(t, o.steps), st, sum, (T*)nullptr, pitch, first,
-                                      (const typename Types<T>::Sum*)nullptr, (const typename Types<T>::Sum*)nullptr);
+                                      (const typename Types<T>::Sum*)nullptr, Upstream<typename Types<T>::Sum>{});
     });
 }
 
@@ -1368,11 +1454,15 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
         return hipSuccess;
     }
     S *up = reinterpret_cast<S*>(ws + p.off_up), *scaling = up + p.T, *dh = reinterpret_cast<S*>(ws + p.off_dh);
+    int* exps = reinterpret_cast<int*>(ws + p.off_exps);
+    Upstream<S> rows_up{up, p.narrow ? nullptr : exps, exps + p.T, scaling, scaling + 1};
     // 16-bit types: g, w and h are turned on their way to the registers; others: copies of them are
     constexpr bool kTurned = sizeof(T) == 2;
     T *ht = reinterpret_cast<T*>(ws + p.off_ht), *wt = reinterpret_cast<T*>(ws + p.off_wt);
     T *g = reinterpret_cast<T*>(ws + p.off_g), *gt = reinterpret_cast<T*>(ws + p.off_gt);
-    ST_TRY((upstream_kernel<T><<<1, 1024, 0, st>>>(static_cast<const S*>(grad), targets, it, p.T, p.V, reduction, rows, up, scaling)));
+    ST_TRY((upstream_kernel<T><<<1, 1024, 0, st>>>(static_cast<const S*>(grad), targets, it, p.T, p.V, reduction, rows, rows_up)));
+    if (reduction != ST_NONE) rows_up.exps = nullptr;   // (one factor for all rows)
+    const Upstream<S> all{};
     if (p.narrow) {
         S *z = reinterpret_cast<S*>(ws + p.off_z), *gs = reinterpret_cast<S*>(ws + p.off_g), *dw = reinterpret_cast<S*>(ws + p.off_dw);
         ST_TRY((narrow_logits_kernel<T><<<dim3((unsigned)((p.T + 63) / 64), (unsigned)p.narrow_parts), kThreads, 0, st>>>(h, w, p.T, (int)p.V, p.D,
@@ -1385,21 +1475,23 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
             h, w, gs, up, scaling, p.T, p.narrow_rows, (int)p.V, p.D, grad_h, grad_w ? dw : nullptr)));
         if (grad_w)
             ST_TRY((finish_kernel<T><<<blocks_for((p.V * p.D + 3) / 4), 256, 0, st>>>(dw, p.narrow_ranges, p.V * p.D, scaling, grad_w, p.D,
-                                                                                     nullptr)));
+                                                                                     all)));
         return hipSuccess;
     }
     const T* hs;
     int64_t h_pitch = p.Dp;
     hipError_t e = in_steps(h, p.T, p.T, p.D, &h_pitch, ws + p.off_h, &hs, false, st);
     if (e != hipSuccess) return e;
-    auto turn = [&](const T* src, T* dst, int64_t r, int64_t pitch, const S* only) -> hipError_t {
+    auto turn = [&](const T* src, T* dst, int64_t r, int64_t pitch, Upstream<S> u) -> hipError_t {
         const dim3 grid((unsigned)((pitch + 63) / 64), (unsigned)((p.D + kTurnCols<T> - 1) / kTurnCols<T>));
-        ST_TRY((transpose_kernel<T><<<grid, 256, 0, st>>>(src, dst, r, p.D, pitch, only)));
+        ST_TRY((transpose_kernel<T><<<grid, 256, 0, st>>>(src, dst, r, p.D, pitch, u)));
         return hipSuccess;
     };
-    if (grad_w && !kTurned && (e = turn(h, ht, p.T, p.Tp, up)) != hipSuccess) return e;
+    if (grad_w && std::is_same_v<T, f16> && rows_up.exps)
+        ST_TRY((largest_kernel<T><<<(unsigned)std::min<int64_t>((p.T + 3) / 4, 2048), kThreads, 0, st>>>(h, p.T, p.D, rows_up)));
+    if (grad_w && !kTurned && (e = turn(h, ht, p.T, p.Tp, rows_up)) != hipSuccess) return e;
     if (grad_w && kTurned)
-        ST_TRY((pack_kernel<T><<<blocks_for(p.Tp * (p.Dp / kPer16<T>)), 256, 0, st>>>(h, ht, p.T, p.Tp, p.D, p.Dp, up)));
+        ST_TRY((pack_kernel<T><<<blocks_for(p.Tp * (p.Dp / kPer16<T>)), 256, 0, st>>>(h, ht, p.T, p.Tp, p.D, p.Dp, rows_up)));
     for (int64_t i = 0; i < p.pieces; ++i) {
         const int64_t first = i * p.piece, n = p.V - first < p.piece ? p.V - first : p.piece;
         const int64_t per = kStepBytes / (int64_t)sizeof(T), np = (n + per - 1) / per * per;
@@ -1427,10 +1519,10 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
                 if (wsrc == w + first * p.D && n != np) {   // (behind the caller's last row nothing may be read)
                     o.a_tail = reinterpret_cast<const char*>(wt);
                     const int64_t whole = np - per;
-                    ST_TRY((pack_kernel<T><<<blocks_for(per * (pitch / kPer16<T>)), 256, 0, st>>>(wsrc + whole * pitch, wt, n - whole, per, p.D, pitch, nullptr)));
+                    ST_TRY((pack_kernel<T><<<blocks_for(per * (pitch / kPer16<T>)), 256, 0, st>>>(wsrc + whole * pitch, wt, n - whole, per, p.D, pitch, all)));
                 }
             } else {
-                if ((e = turn(w + first * p.D, wt, n, np, nullptr)) != hipSuccess) return e;
+                if ((e = turn(w + first * p.D, wt, n, np, all)) != hipSuccess) return e;
                 o = operands(wt, np, p.D, g, np, p.T, np);
             }
             if (p.sums) e = launch_sums<T, kTurned, false>(o, p.by_h, dh, p.D, i == 0, st);
@@ -1438,7 +1530,7 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
                 e = with_sub<T>(p.by_h.sub, [&](auto sub) {
                     constexpr int SUB = decltype(sub)::value;
                     return launch_product<T, SUB>(product_kernel<T, SUB, false, kTurned, false>, o, 1, st, (S*)nullptr, grad_h, p.D, true, (const S*)scaling,
-                                                   (const S*)up);
+                                                   rows_up);
                 });
             if (e != hipSuccess) return e;
         }
@@ -1447,20 +1539,20 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
             if (p.by_w.parts > 1) {
                 S* dw = reinterpret_cast<S*>(ws + p.off_dw);
                 if ((e = launch_sums<T, kTurned, kTurned>(o, p.by_w, dw, p.D, true, st)) != hipSuccess) return e;
-                ST_TRY((finish_kernel<T><<<blocks_for((n * p.D + 3) / 4), 256, 0, st>>>(dw, p.by_w.parts, n * p.D, scaling, grad_w + first * p.D, p.D,
-                                                                                            nullptr)));
+                ST_TRY((finish_kernel<T><<<blocks_for((n * p.D + 3) / 4), 256, 0, st>>>(dw, p.by_w.parts, n * p.D, scaling + 1, grad_w + first * p.D,
+                                                                                            p.D, all)));
                 continue;
             }
             e = with_sub<T>(p.by_w.sub, [&](auto sub) {
                 constexpr int SUB = decltype(sub)::value;
                 return launch_product<T, SUB>(product_kernel<T, SUB, false, kTurned, kTurned>, o, 1, st, (S*)nullptr, grad_w + first * p.D, p.D, true,
-                                              (const S*)scaling, (const S*)nullptr);
+                                              (const S*)scaling + 1, all);
             });
             if (e != hipSuccess) return e;
         }
     }
     if (grad_h && p.sums)
-        ST_TRY((finish_kernel<T><<<blocks_for((p.T * p.D + 3) / 4), 256, 0, st>>>(dh, p.by_h.parts, p.T * p.D, scaling, grad_h, p.D, up)));
+        ST_TRY((finish_kernel<T><<<blocks_for((p.T * p.D + 3) / 4), 256, 0, st>>>(dh, p.by_h.parts, p.T * p.D, scaling, grad_h, p.D, rows_up)));
     return hipSuccess;
 }
 

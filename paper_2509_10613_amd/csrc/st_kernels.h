@@ -59,6 +59,7 @@ struct EntropyPlan {
     size_t off_max, off_sum, off_hit;   // forward: running maximum and sum, and the target's logit, of every row
     size_t off_part;           // ... and those of the piece's tiles
     size_t off_up;             // backward: every row's upstream gradient (and behind them the scaling, two numbers)
+    size_t off_exps;           // ... and the powers of two that stay out of it (and behind them the largest of h's)
     size_t off_ht, off_wt;     // ... h and a piece of w transposed; 16-bit types: h without rows that have no target, and w's last step
     size_t off_g, off_gt;      // ... the piece's gradients of the logits, as they are and (not of 16-bit types) transposed
     size_t off_dh, off_dw;     // ... the sums of grad_h, and of a piece's grad_w, one per part
