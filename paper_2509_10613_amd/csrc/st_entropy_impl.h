@@ -481,11 +481,17 @@ __device__ __forceinline__ void times_power(Vec<T, E>& v, S, int e)
     for (int i = 0; i < E; ++i) v.v[i] = (T)power((S)v.v[i], e);
 }
 
-// A result in the arrays' type, f 2^e x; a 0 stays one whatever is upstream (rows without a target).
+// A result in the arrays' type; a 0 stays one whatever is upstream (rows without a target).
+template <typename T, typename S>
+__device__ __forceinline__ T scaled(S x, S f)
+{
+    return (T)(x == 0 ? x : x * f);
+}
+// ... f 2^e x
 template <typename T, typename S>
 __device__ __forceinline__ T scaled(S x, S f, int e)
 {
-    return (T)(x == 0 ? x : power(x * f, e));
+    return (T)power(x == 0 ? x : x * f, e);
 }
 struct NoOutbox {
     char* lds;
@@ -832,7 +838,11 @@ __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void product_kernel(Ope
             } else {
                 Vec<T, 4> v;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v.v[r] = none ? T(0) : scaled<T>(x.v[r], f, e);
+                for (int r = 0; r < 4; ++r) v.v[r] = scaled<T>(x.v[r], f);
+                if (rows.exps)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v.v[r] = scaled<T>(x.v[r], f, e);
+                if (none) v = Vec<T, 4>{};
                 if constexpr (sizeof(T) == 2) outbox.put(wn * kWave + j * 16 + (lane & 15), col, v);
                 else if (kApart == 1 && m + 3 < o.m) store_vec(out + at, v);
                 else
@@ -865,15 +875,19 @@ __global__ __launch_bounds__(256) void finish_kernel(const typename Types<T>::Su
         }
         Vec<T, E> v;
 #pragma unroll
-        for (int e = 0; e < E; ++e) v.v[e] = scaled<T>(x.v[e], f, 0);
+        for (int e = 0; e < E; ++e) v.v[e] = scaled<T>(x.v[e], f);
         if (rows.up) {
-            int64_t row = i / D, left = D - (i - row * D);
+            int64_t row = (uint64_t)entries >> 32 ? i / D : (int64_t)((uint32_t)i / (uint32_t)D), left = D - (i - row * D);
+            if (left >= E && !rows.exps) {   // one row, as most
+                if (rows.up[row] == 0) v = Vec<T, E>{};
+            } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (e < n) v.v[e] = rows.up[row] == 0 ? T(0) : scaled<T>(x.v[e], f, rows.exponent(row));
-                if (--left == 0) {
-                    ++row;
-                    left = D;
+                for (int e = 0; e < E; ++e) {
+                    if (e < n) v.v[e] = rows.up[row] == 0 ? T(0) : scaled<T>(x.v[e], f, rows.exponent(row));
+                    if (--left == 0) {
+                        ++row;
+                        left = D;
+                    }
                 }
             }
         }
@@ -1027,7 +1041,7 @@ __global__ __launch_bounds__(kThreads) void narrow_grads_kernel(const T* __restr
             if (grad_h) {
                 Vec<T, E> out;
 #pragma unroll
-                for (int e = 0; e < E; ++e) out.v[e] = scaled<T>(y[e], f, 0);
+                for (int e = 0; e < E; ++e) out.v[e] = scaled<T>(y[e], f);
                 if (width == E) store_vec(grad_h + (t + i) * D + col, out);
                 else store_some(grad_h + (t + i) * D + col, out, width);
             }
