@@ -73,9 +73,10 @@ int sigtrain_entropy_bwd(const void* h, const void* w, const void* targets, cons
 
 /*
  * *norm = sqrt(sum of the squares of all entries of `n` arrays): grads[i] (device) of counts[i] entries of type dts[i]; the three
- * lists are host memory and free again when the call returns.  Squares and sums are in double.
+ * lists are host memory and free again when the call returns.  Squares and sums are in double (doubles beyond 1e154 have an infinite norm).
  *
- * sigtrain_clip also writes out[i] = grads[i] * min(1, max_norm / *norm), rounded once to out_dts[i].  out[i] may be grads[i]
+ * sigtrain_clip also writes out[i] = grads[i] * min(1, max_norm / *norm), rounded once to out_dts[i] from a product in double (in float where
+ * neither side has more than 32 bits, the entries have 16 and the factor is a normal float).  out[i] may be grads[i]
  * (then out_dts[i] = dts[i]); otherwise no output may overlap an input or another output (SK_ERR_SHAPE).  If the norm is
  * infinite or NaN the entries are passed on as they are: *norm says so.  max_norm >= 0.
  */

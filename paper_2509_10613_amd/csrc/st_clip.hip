@@ -87,11 +87,10 @@ __device__ __forceinline__ double squares(const T* p, int n)
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
-template <typename T, typename O, int THREADS>
+// A: the product's type.
+template <typename T, typename O, typename A, int THREADS>
 __device__ __forceinline__ void scale(const T* p, O* q, int n, double factor)
 {
-    // float and double: the product in double, rounded once; of 16-bit entries in float, which is within 2^-23 of it
-    using A = sum_t<T>;
     constexpr int E = kPer16<T>, U = 2;
     const A f = (A)factor;
     const bool same = factor == 1.0;
@@ -137,7 +136,13 @@ __device__ __forceinline__ void chunk_scale(const Batch& b, uint32_t c, double f
         by_type(b.out_dt[a], [&](auto out_type) {
             using T = decltype(type);
             using O = decltype(out_type);
-            scale<T, O, THREADS>(static_cast<const T*>(b.in[a]) + first, static_cast<O*>(b.out[a]) + first, n, factor);
+            const T* from = static_cast<const T*>(b.in[a]) + first;
+            O* to = static_cast<O*>(b.out[a]) + first;
+            // The product in double, rounded once; of 16-bit entries that do not become doubles in float, which is within 2^-23 of it, unless
+            // the factor is below float's normal numbers (entries near 1e38 of bfloat16).
+            if constexpr (sizeof(T) == 2 && sizeof(O) != 8)
+                if (factor >= __FLT_MIN__) return scale<T, O, float, THREADS>(from, to, n, factor);
+            scale<T, O, double, THREADS>(from, to, n, factor);
         });
     });
 }
