@@ -28,8 +28,8 @@ typedef enum { ST_I32 = 0, ST_I64 = 1 } st_itype;
 
 /*
  * out[n, :] = scale * table[tokens[n], :] for tokens[count], table[V, D], out[count, D].  A token outside 0 .. V - 1 stands for
- * no symbol (padding): its row is 0, and it takes no part in the gradient.  The product is formed in float (double for ST_F32 and
- * ST_F64) and rounded once.
+ * no symbol (padding): its row is 0, and it takes no part in the gradient.  The product is formed in float (double for ST_F32, ST_F64
+ * and scales that are no normal float) and rounded once.
  */
 int sigtrain_embed_fwd(const void* tokens, const void* table, void* out, int64_t count, int64_t V, int64_t D, double scale,
                        st_itype it, st_dtype dt, void* stream);

@@ -11,6 +11,9 @@
 // begins in the sorted symbols is found by a search on the diagonal i + key[i].  A row whose events are spread over several
 // units is finished by a second launch from what they hand over, in their order.  Bound by memory as well: 131072 rows of 4096 bfloat16 from 8192
 // tokens 215 us (5.3 TB/s), 50257 rows of 1024 floats from 262144 tokens 290 us (4.4 TB/s); the sort takes 20 and 54 us of that call, the joins 12 and 38.
+#include <cfloat>
+#include <cmath>
+
 #include "st_dev.h"
 #include "st_kernels.h"
 
@@ -23,7 +26,7 @@ constexpr int kThreads = 256;
 // A lane moves U vectors of E entries (16 bytes where a row has as much), all symbols loaded before the first row and all rows before the first
 // store: no branch stands between them.  A row's last vector ends with the row, whatever its length: it may write entries of the one before a second
 // time, with the same values.
-// A: the product's type, double unless the scale is a float (then a float's product, rounded once, is the same number).
+// A: the product's type, double unless the scale is a float (then a float's product, rounded once, is the same number); of 16-bit types float.
 // Index: uint32_t where the number of vectors allows (a 32-bit division per vector instead of a 64-bit one).
 template <typename T, typename A, typename Index, int E, int U>
 __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(const void* tokens, int it, const T* table, T* out, int64_t V, int64_t D, A scale,
@@ -344,9 +347,10 @@ struct Handed {
     Listed* list[2];       // short, long
 };
 
-template <typename T>
+// P: the type of a sum's product with the scale.
+template <typename T, typename P>
 __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const T* grad, T* out, const uint32_t* keys, const uint32_t* places, int64_t n,
-                                                              int64_t V, int64_t D, int lanes, int events, sum_t<T> scale,
+                                                              int64_t V, int64_t D, int lanes, int events, P scale,
                                                               Handed<sum_t<T>> handed)
 {
     constexpr int E = kPer16<T>, kAhead = 8;
@@ -435,7 +439,7 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(const T* grad, T* 
             } else if (width > 0) {
                 Vec<T, E> r;
 #pragma unroll
-                for (int i = 0; i < E; ++i) r.v[i] = (T)(sum[i] * scale);
+                for (int i = 0; i < E; ++i) r.v[i] = (T)((P)sum[i] * scale);
                 if (width == E) store_vec(to, r);
                 else store_some(to, r, width);
             }
@@ -484,8 +488,8 @@ __device__ __forceinline__ A carried(const A* carry, int64_t from, int64_t to, i
     for (; i < to; ++i) sum += carry[i * D + c];
     return sum;
 }
-template <typename T>
-__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(T* out, const uint32_t* keys, int64_t D, int events, sum_t<T> scale,
+template <typename T, typename P>
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(T* out, const uint32_t* keys, int64_t D, int events, P scale,
                                                                      Handed<sum_t<T>> handed)
 {
     using A = sum_t<T>;
@@ -516,7 +520,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(T* out, con
         if (!is_long) {
             const int64_t c0 = (int64_t)((task - many) % shares) * kShare, c1 = c0 + kShare < D ? c0 + kShare : D;
             for (int64_t c = c0 + threadIdx.x; c < c1; c += 64 * kJoinWaves)
-                out[row * D + c] = (T)((carried(handed.carry, first, u, D, c) + handed.head[u * D + c]) * scale);
+                out[row * D + c] = (T)((P)(carried(handed.carry, first, u, D, c) + handed.head[u * D + c]) * scale);
             continue;
         }
         const int64_t c = (int64_t)(task % slices) * 64 + lane;
@@ -526,7 +530,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(T* out, con
             A all = 0;
 #pragma unroll
             for (int j = 0; j < kJoinWaves; ++j) all += parts[j][lane];
-            out[row * D + c] = (T)((all + handed.head[u * D + c]) * scale);
+            out[row * D + c] = (T)((P)(all + handed.head[u * D + c]) * scale);
         }
         __syncthreads();
     }
@@ -542,6 +546,9 @@ hipError_t by_type(int dt, F&& f)
     default: return f(f16{});
     }
 }
+
+// Whether a float holds the scale as well as any other: outside its normal numbers 0 times it may be NaN, and others' products 0.
+bool float_scale(double scale) { return scale == 0 || (std::fabs(scale) >= FLT_MIN && std::fabs(scale) <= FLT_MAX); }
 
 }  // namespace
 
@@ -566,9 +573,12 @@ hipError_t embed_fwd(const void* tokens, const void* table, void* out, int64_t c
                 if (D >= 2) return run_fwd<T, A, 2>(tokens, from, to, count, V, D, scale, it, st);
             return run_fwd<T, A, 1>(tokens, from, to, count, V, D, scale, it, st);
         };
-        if constexpr (sizeof(T) == 4)
+        if constexpr (sizeof(T) == 4) {
             if ((double)(float)scale == scale) return by_width(float{});
-        return by_width(sum_t<T>{});
+        } else if constexpr (sizeof(T) == 2) {
+            if (float_scale(scale)) return by_width(float{});
+        }
+        return by_width(double{});
     });
 }
 
@@ -654,16 +664,22 @@ hipError_t embed_bwd(const EmbedPlan& p, const void* tokens, const void* grad_ou
         const Handed<A> handed{reinterpret_cast<A*>(base + p.off_carry), reinterpret_cast<A*>(base + p.off_head), list,
                                {reinterpret_cast<Listed*>(list + 64), reinterpret_cast<Listed*>(list + 64) + p.units}};
         const size_t lds = (size_t)(kThreads / p.lanes) * p.events * 4;
-        embed_sums_kernel<T><<<dim3((unsigned)p.groups, p.slices), kThreads, lds, st>>>(
-            static_cast<const T*>(grad_out), static_cast<T*>(grad_table), keys[from], places[from], p.count, p.V, p.D, p.lanes, p.events,
-            (A)scale, handed);
-        hipError_t err = hipGetLastError();
-        if (err != hipSuccess || p.count == 0) return err;
-        // (as many workgroups as run at once take the list in turns)
-        const int64_t most = p.units * 2;
-        embed_join_kernel<T><<<(unsigned)(most < 2048 ? most : 2048), 64 * kJoinWaves, 0, st>>>(static_cast<T*>(grad_table), keys[from], p.D, p.events, (A)scale,
-                                                                                             handed);
-        return hipGetLastError();
+        auto sums = [&](auto factor) {
+            using P = decltype(factor);
+            embed_sums_kernel<T, P><<<dim3((unsigned)p.groups, p.slices), kThreads, lds, st>>>(
+                static_cast<const T*>(grad_out), static_cast<T*>(grad_table), keys[from], places[from], p.count, p.V, p.D, p.lanes, p.events, factor,
+                handed);
+            const hipError_t err = hipGetLastError();
+            if (err != hipSuccess || p.count == 0) return err;
+            // (as many workgroups as run at once take the list in turns)
+            const int64_t most = p.units * 2;
+            embed_join_kernel<T, P><<<(unsigned)(most < 2048 ? most : 2048), 64 * kJoinWaves, 0, st>>>(static_cast<T*>(grad_table), keys[from], p.D, p.events,
+                                                                                                    factor, handed);
+            return hipGetLastError();
+        };
+        if constexpr (sizeof(T) == 2)
+            if (float_scale(scale)) return sums((float)scale);
+        return sums(scale);
     });
 }
 
