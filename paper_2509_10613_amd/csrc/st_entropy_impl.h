@@ -1086,7 +1086,8 @@ __global__ __launch_bounds__(256) void zero_kernel(T* p, int64_t n)
 }
 
 // dst[cols][pitch] = src[rows][cols] transposed, zeros behind the rows.  `u`: as in pack_kernel.
-// A workgroup turns 64 x 64 entries (32 x 64 of double), moved as 16 bytes either way.
+// A workgroup turns 64 x 64 entries (32 x 64 of double), moved as 16 bytes either way.  All tiles are the grid's first index: there may be more than 65536
+// along either side.
 template <typename T>
 constexpr int kTurnCols = sizeof(T) == 8 ? 32 : 64;
 template <typename T>
@@ -1094,11 +1095,12 @@ __global__ __launch_bounds__(256) void transpose_kernel(const T* src, T* dst, in
                                                         Upstream<typename Types<T>::Sum> u)
 {
     using S = typename Types<T>::Sum;
-    if (u.exps && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) u.put_w_unscale();
+    if (u.exps && blockIdx.x == 0 && threadIdx.x == 0) u.put_w_unscale();
     const int shift = u.exps ? u.shift() : 0;
     constexpr int R = 64, C = kTurnCols<T>, E = kPer16<T>, kPad = 4 / sizeof(T) ? 4 / sizeof(T) : 1;
     __shared__ T tile[C][R + kPad];   // (an odd number of words from column to column, or of double words)
-    const int64_t r0 = (int64_t)blockIdx.x * R, c0 = (int64_t)blockIdx.y * C;
+    const uint32_t across = (uint32_t)((pitch + R - 1) / R), down = blockIdx.x / across;
+    const int64_t r0 = (int64_t)(blockIdx.x - down * across) * R, c0 = (int64_t)down * C;
     for (int i = threadIdx.x; i < R * C / E; i += 256) {
         const int row = i / (C / E), col = i % (C / E) * E;
         const int64_t r = r0 + row, left = cols - c0 - col;
@@ -1497,8 +1499,8 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
     hipError_t e = in_steps(h, p.T, p.T, p.D, &h_pitch, ws + p.off_h, &hs, false, st);
     if (e != hipSuccess) return e;
     auto turn = [&](const T* src, T* dst, int64_t r, int64_t pitch, Upstream<S> u) -> hipError_t {
-        const dim3 grid((unsigned)((pitch + 63) / 64), (unsigned)((p.D + kTurnCols<T> - 1) / kTurnCols<T>));
-        ST_TRY((transpose_kernel<T><<<grid, 256, 0, st>>>(src, dst, r, p.D, pitch, u)));
+        const int64_t tiles = (pitch + 63) / 64 * ((p.D + kTurnCols<T> - 1) / kTurnCols<T>);
+        ST_TRY((transpose_kernel<T><<<(unsigned)tiles, 256, 0, st>>>(src, dst, r, p.D, pitch, u)));
         return hipSuccess;
     };
     if (grad_w && std::is_same_v<T, f16> && rows_up.exps)
