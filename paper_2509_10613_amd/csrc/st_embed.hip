@@ -27,18 +27,18 @@ constexpr int kThreads = 256;
 // store: no branch stands between them.  A row's last vector ends with the row, whatever its length: it may write entries of the one before a second
 // time, with the same values.
 // A: the product's type, double unless the scale is a float (then a float's product, rounded once, is the same number); of 16-bit types float.
-// Index: uint32_t where the number of vectors allows (a 32-bit division per vector instead of a 64-bit one).
-template <typename T, typename A, typename Index, int E, int U>
+// items: fewer than 2^31 vectors (a 32-bit division for each).
+template <typename T, typename A, int E, int U>
 __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(const void* tokens, int it, const T* table, T* out, int64_t V, int64_t D, A scale,
-                                                             Index per_row, Index items)
+                                                             uint32_t per_row, uint32_t items)
 {
-    const Index first = (Index)blockIdx.x * (kThreads * U) + threadIdx.x;
+    const uint32_t first = blockIdx.x * (kThreads * U) + threadIdx.x;
     int64_t symbol[U], at[U];
     int64_t col[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const Index item = first + u * kThreads < items ? first + u * kThreads : items - 1;
-        const Index row = item / per_row;
+        const uint32_t item = first + u * kThreads < items ? first + u * kThreads : items - 1;
+        const uint32_t row = item / per_row;
         const int64_t c = (int64_t)(item - row * per_row) * E;
         col[u] = c <= D - E ? c : D - E;
         at[u] = (int64_t)row * D + col[u];
@@ -66,17 +66,21 @@ __global__ __launch_bounds__(kThreads) void zeros_kernel(T* out, int64_t n)
 template <typename T, typename A, int E>
 hipError_t run_fwd(const void* tokens, const T* table, T* out, int64_t count, int64_t V, int64_t D, double scale, int it, hipStream_t st)
 {
-    const int64_t per_row = (D + E - 1) / E, items = count * per_row;
+    const int64_t per_row = (D + E - 1) / E, most = (((int64_t)1 << 31) - 1) / per_row;   // (rows of at most 2^24 entries)
     const A f = (A)scale;
-    // four vectors per lane; one where that leaves compute units idle (2^41 entries at most: a grid holds their vectors)
-    auto blocks = [&](int64_t vectors) { return (unsigned)((items + vectors - 1) / vectors); };
-    if (items < (int64_t)kThreads * 2048)
-        embed_fwd_kernel<T, A, uint32_t, E, 1><<<blocks(kThreads), kThreads, 0, st>>>(tokens, it, table, out, V, D, f, (uint32_t)per_row, (uint32_t)items);
-    else if (items < (int64_t)1 << 31)
-        embed_fwd_kernel<T, A, uint32_t, E, 4><<<blocks(kThreads * 4), kThreads, 0, st>>>(tokens, it, table, out, V, D, f, (uint32_t)per_row, (uint32_t)items);
-    else
-        embed_fwd_kernel<T, A, uint64_t, E, 4><<<blocks(kThreads * 4), kThreads, 0, st>>>(tokens, it, table, out, V, D, f, (uint64_t)per_row, (uint64_t)items);
-    return hipGetLastError();
+    for (int64_t row = 0; row < count; row += most) {   // a launch has at most 2^32 threads
+        const int64_t items = (count - row < most ? count - row : most) * per_row;
+        const void* from = static_cast<const char*>(tokens) + row * (it == ST_I32 ? 4 : 8);
+        // four vectors per lane; one where that leaves compute units idle
+        auto launch = [&](auto kernel, int64_t vectors) {
+            kernel<<<(unsigned)((items + vectors - 1) / vectors), kThreads, 0, st>>>(from, it, table, out + row * D, V, D, f, (uint32_t)per_row,
+                                                                                  (uint32_t)items);
+            return hipGetLastError();
+        };
+        const hipError_t e = items < (int64_t)kThreads * 2048 ? launch(embed_fwd_kernel<T, A, E, 1>, kThreads) : launch(embed_fwd_kernel<T, A, E, 4>, kThreads * 4);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // ------------------------------------------------------------------------------------------------ sort
