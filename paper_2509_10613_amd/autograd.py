@@ -298,16 +298,55 @@ def grad_norm(grads):
     return sk.grad_norm([g.detach().contiguous() for g in grads]) if norm is None else norm
 
 
+def _reaches(total, axes, budget):
+    """Whether the sum of stride * x over axes (stride, most), the largest strides first, is `total` for some 0 <= x <= most; at most budget[0] steps
+    (after that no)."""
+    budget[0] -= 1
+    if total == 0:
+        return True
+    if not axes or budget[0] < 0:
+        return False
+    (s, most), rest = axes[0], axes[1:]
+    short = total - sum(t * n for t, n in rest)   # what x has to make up for at least
+    return any(_reaches(total - s * x, rest, budget) for x in range(max(0, -(-short // s)), min(most, total // s) + 1))
+
+
+def _refuse_shared(outs):
+    """An error if two tensors that are to be written share memory, or one has an entry more than once: what the library refuses of contiguous arrays,
+    for other layouts."""
+    spans = []
+    for i, t in enumerate(outs):
+        if t.numel() == 0:
+            continue
+        axes = [(s * t.element_size(), n - 1) for s, n in zip(t.stride(), t.shape) if n > 1] + [(1, t.element_size() - 1)]
+        if any(s == 0 for s, _ in axes):
+            raise ValueError("tensor %d has entries that share memory" % i)
+        spans.append((t.data_ptr(), t.data_ptr() + 1 + sum(s * n for s, n in axes), axes, i))
+    spans.sort(key=lambda span: span[0])
+    for j, (a0, a1, a_axes, a) in enumerate(spans):
+        for b0, b1, b_axes, b in spans[j + 1:]:
+            if b0 >= a1:
+                break
+            # a byte of both: a0 + (steps along a) = b0 + (steps along b), the latter counted from their ends
+            joined = {}
+            for s, n in a_axes + b_axes:
+                joined[s] = joined.get(s, 0) + n
+            if _reaches(b1 - 1 - a0, sorted(joined.items(), reverse=True), [100000]):
+                raise sk.SigKernelError("the output of array %d overlaps another array, or the other way round" % max(a, b))
+
+
 def clip_grad_norm(grads, max_norm, out=None):
     """Scales a tensor or several, taken together, down to the norm `max_norm` where theirs is larger, in place, or into the tensors
     `out` (which may be of other floating types: the optimizer's copies); returns their norm, a float64 [] on the device, without waiting
-    for it.  Tensors whose norm is infinite or NaN are left (passed on) as they are.  No tensor may come twice in place.  Tensors of
-    other layouts than contiguous ones go through copies."""
+    for it.  Tensors whose norm is infinite or NaN are left (passed on) as they are.  Tensors
+    that are written may not share entries.  Tensors of other layouts than contiguous ones go through copies."""
     grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
     outs = grads if out is None else ([out] if isinstance(out, torch.Tensor) else list(out))
     norm = _native.clip(grads, outs, float(max_norm))
     if norm is not None:
         return norm
+    if not all(o.is_contiguous() for o in outs):
+        _refuse_shared(outs)
     with torch.no_grad():
         dense = [g.contiguous() for g in grads]
         if out is None:
