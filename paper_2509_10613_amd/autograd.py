@@ -279,7 +279,7 @@ def linear_cross_entropy(h, weight, targets, reduction="mean"):
     """Softmax cross entropy of the logits h weight^T, h[..., D], weight[V, D], targets[...]: the mean over the rows with a target (0 if there
     are none), the sum, or with "none" every row's; differentiable in h and weight.  The logits of all classes never exist at
     once, forward or backward.  A row whose target is outside 0 .. V - 1 has none: its loss and its gradient are 0, and what it holds
-    reaches nothing.  float32 (float64 for float64 arrays)."""
+    reaches nothing; with "none" a row whose upstream gradient is 0 takes no part in the gradients either.  float32 (float64 for float64 arrays)."""
     if isinstance(reduction, str):
         loss = _native.entropy(h, weight, targets, reduction)
         if loss is not None:
@@ -292,7 +292,7 @@ def linear_cross_entropy(h, weight, targets, reduction="mean"):
 
 def grad_norm(grads):
     """The Euclidean norm of all entries of a tensor or of several (of any floating types and layouts, on one device), as a float64 [] on
-    the device."""
+    the device.  Squares are summed in float64: infinite for float64 entries beyond 1e154."""
     grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
     norm = _native.clip(grads, None, 0.0)
     return sk.grad_norm([g.detach().contiguous() for g in grads]) if norm is None else norm

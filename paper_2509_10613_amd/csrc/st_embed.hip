@@ -10,7 +10,7 @@
 // consecutive events, so that neither a frequent symbol nor a stretch of absent ones makes one unit work longer; where a unit
 // begins in the sorted symbols is found by a search on the diagonal i + key[i].  A row whose events are spread over several
 // units is finished by a second launch from what they hand over, in their order.  Bound by memory as well: 131072 rows of 4096 bfloat16 from 8192
-// tokens 215 us (5.3 TB/s), 50257 rows of 1024 floats from 262144 tokens 290 us (4.4 TB/s); the sort takes 20 and 54 us of that call, the joins 12 and 38.
+// tokens 215 us (5.3 TB/s), 50257 rows of 1024 floats from 262144 tokens 290 us (4.4 TB/s); the sort takes 20 and 54 us of that call, the joins 13 and 38.
 #include <cfloat>
 #include <cmath>
 

@@ -106,8 +106,11 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
         p.total = std::max<size_t>(at, 256);
     };
     const int64_t all = (V + kTileRows - 1) / kTileRows * kTileRows;
-    // Few classes of wide rows (1000 rows of 37449 floats, ten classes: loss 117 us by tiles and 42 like this, with gradients 448 and 231; narrow rows
-    // would leave most lanes of the gradients' kernel idle).  Ranges of 48 rows at least: their sums of grad_w are added up by one launch.
+    // Few classes of wide rows.  By tiles and like this, loss and gradients, ten classes: 1000 rows of 37449 floats 458 and 222 us (loss 105 and 41), of 5461
+    // doubles 161 and 98, of 512 floats 97 and 87 (256 floats: 92 and 89, most lanes of the gradients' kernel idle; the other way for 4000 rows of 2000
+    // bfloat16 and 16 classes, 103 and 124).  The loss of at most 16 rows goes to the kernel for those, whose workgroups are the classes' alone: of ten classes that
+    // is one, 195 to 259 us for 1 to 16 rows of 37449 floats where this would take 25 (1000 floats: 23 and 25).  Ranges of 48 rows at least: their sums
+    // of grad_w are added up by one launch.
     if (V <= 16 && D >= 512 && (backward || T > 16)) {
         p.narrow = true;
         p.piece = all;
@@ -148,7 +151,7 @@ EntropyPlan entropy_plan(bool backward, int64_t T, int64_t V, int64_t D, int dt,
     const int64_t each = backward ? (p.size == 2 ? 1 : 2) * (p.Tp + p.Dp) * p.size : (T <= 16 ? 0 : p.Dp * p.size) + 2 * T * p.sum_size / 64 + 1;
     int64_t most = ((int64_t)1 << 30) / each / kTileRows;
     if (most < 1) most = 1;
-    if (most > (1 << 14)) most = 1 << 14;   // (tiles of a piece are a grid's second index)
+    if (most > (1 << 14)) most = 1 << 14;   // (2^22 classes: a tile's 128 rows of that many doubles lie within 32-bit offsets)
     if (most > all / kTileRows) most = all / kTileRows;
     auto fits = [&](int64_t rows) {
         lay(rows * kTileRows);

@@ -2,8 +2,8 @@
 //
 // Forward: the logits z = h w^T are formed tile by tile on the matrix cores and reduced in registers to every row's maximum and sum
 // of exponentials over the tile (and the target's logit); no logit is written.  Backward: the logits of a piece of the classes are formed
-// again, their gradients G = u (exp(z - lse) - [class = target]) rounded to the arrays' type and written, and multiplied: grad_h += G w and
-// grad_w = G^T h.  The floor is the products: 2 T V D operations for the loss, 4 T V D for the gradients and, since the logits are not kept, 2 T V D
+// again, their gradients G = u (exp(z - lse) - [class = target]) rounded to the arrays' type and written (what of u stays out of them:
+// upstream_kernel), and multiplied: grad_h += G w and grad_w = G^T h.  The floor is the products: 2 T V D operations for the loss, 4 T V D for the gradients and, since the logits are not kept, 2 T V D
 // once more.  8192 rows, 4096 channels, 131072 classes in bfloat16: 27.7 ms in all, forward 6.8 (1300 TFLOP/s), logits and their gradients 7.7,
 // grad_h 6.6, grad_w 6.7 (1320); a large library product reaches 1150 to 1440 on this card.
 //
@@ -500,7 +500,8 @@ template <typename T, int TILE>
 using OutboxOf = typename std::conditional_t<sizeof(T) == 2, std::enable_if<true, Outbox<std::conditional_t<sizeof(T) == 2, T, bf16>, TILE>>,
                                              std::enable_if<true, NoOutbox>>::type;
 
-// Forward: every row's maximum and sum of exponentials over the tile's classes (A: classes of w, B: rows of h).
+// Forward: every row's maximum and sum of exponentials over the tile's classes (A: classes of w, B: rows of h).  (Of 16-bit types with the largest tile
+// 24 registers are kept in scratch memory, 52 bytes a lane, besides 256 of each file; no other of these kernels does.)
 template <typename T, int SUB>
 __global__ __launch_bounds__(kThreads, SUB == 8 ? 1 : 2) void stats_kernel(Operands o, TileOrder order, const void* targets, int it, int64_t first_class, int64_t V,
                                                          typename Types<T>::Sum* part_max, typename Types<T>::Sum* part_sum,
