@@ -1293,7 +1293,7 @@ __global__ __launch_bounds__(1024) void upstream_kernel(const typename Types<T>:
     }
 }
 
-// The largest exponent among the entries of h, each with its row's power of two.  A wave per row.
+// The largest exponent among the entries of h, each with its row's power of two.  A wave per row, one atomic operation per workgroup.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void largest_kernel(const T* h, int64_t rows, int64_t D, Upstream<typename Types<T>::Sum> u)
 {
@@ -1319,7 +1319,12 @@ __global__ __launch_bounds__(kThreads) void largest_kernel(const T* h, int64_t r
     }
 #pragma unroll
     for (int o = 32; o > 0; o /= 2) largest = max(largest, __shfl_xor(largest, o));
-    if (lane == 0 && largest != INT_MIN) atomicMax(u.largest, largest);   // (a whole number: in any order)
+    __shared__ int waves[4];
+    if (lane == 0) waves[threadIdx.x >> 6] = largest;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int i = 1; i < 4; ++i) largest = max(largest, waves[i]);
+    if (largest != INT_MIN) atomicMax(u.largest, largest);   // (a whole number: in any order)
 }
 
 unsigned blocks_for(int64_t items) { return (unsigned)((items + 255) / 256 < 16384 ? (items + 255) / 256 : 16384); }
@@ -1505,7 +1510,7 @@ hipError_t entropy_run_bwd(const EntropyPlan& p, const T* h, const T* w, const v
         return hipSuccess;
     };
     if (grad_w && std::is_same_v<T, f16> && rows_up.exps)
-        ST_TRY((largest_kernel<T><<<(unsigned)std::min<int64_t>((p.T + 3) / 4, 2048), kThreads, 0, st>>>(h, p.T, p.D, rows_up)));
+        ST_TRY((largest_kernel<T><<<(unsigned)std::min<int64_t>((p.T + 3) / 4, 256), kThreads, 0, st>>>(h, p.T, p.D, rows_up)));
     if (grad_w && !kTurned && (e = turn(h, ht, p.T, p.Tp, rows_up)) != hipSuccess) return e;
     if (grad_w && kTurned)
         ST_TRY((pack_kernel<T><<<blocks_for(p.Tp * (p.Dp / kPer16<T>)), 256, 0, st>>>(h, ht, p.T, p.Tp, p.D, p.Dp, rows_up)));
